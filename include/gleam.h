@@ -421,7 +421,9 @@ int gleam_cache_profile_read(gleam_cache_t* cache, double* h_ms, uint64_t* h_lau
  *
  * The calls are asynchronous on `stream`, run on the current GPU, take device
  * memory only, allocate nothing and keep nothing.  Work that reads or writes
- * their buffers is ordered by the stream. */
+ * their buffers is ordered by the stream: no call lets later work start before
+ * its results are written, so they may be the payload of a call with
+ * GLEAM_OVERLAP_CALLS. */
 
 enum gleam_dtype { GLEAM_BF16 = 0, GLEAM_FP16 = 1, GLEAM_FP32 = 2 };
 

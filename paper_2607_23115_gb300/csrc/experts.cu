@@ -40,7 +40,6 @@ __device__ __forceinline__ uint32_t slot_expert(const SortArgs& a, uint64_t i) {
 __global__ void __launch_bounds__(kSortThreads, 1) k_expert_sort(const __grid_constant__ SortArgs a) {
   extern __shared__ uint32_t hist[];  // [warps][experts]
   __shared__ SortShared sh;
-  pdl_trigger();
   pdl_wait();
   cg::cluster_group cl = cg::this_cluster();
   const uint32_t rank = cl.block_rank(), blocks = cl.num_blocks();
@@ -146,7 +145,6 @@ __device__ __forceinline__ int64_t row_in(int32_t r, uint64_t rows) {
 // Blocks (x: row, y: part of it).
 constexpr int kGatherPieces = 4;  // of a thread
 __global__ void __launch_bounds__(kRowThreads) k_expert_gather(const __grid_constant__ RowsArgs a) {
-  pdl_trigger();
   pdl_wait();
   const int32_t slot = a.src_of[blockIdx.x];
   const int64_t t = slot < 0 ? -1 : row_in((int32_t)((uint32_t)slot / a.per_token), a.a_rows);
@@ -179,7 +177,6 @@ template <int DT>
 __global__ void __launch_bounds__(kRowThreads) k_expert_combine(const __grid_constant__ RowsArgs a) {
   constexpr int kN = Piece<DT>::kValues;
   constexpr uint64_t kSize = dtype_bytes(DT);
-  pdl_trigger();
   pdl_wait();
   const uint64_t t = blockIdx.x;
   const int32_t* row_of = a.row_of + t * a.per_token;
@@ -232,7 +229,6 @@ __global__ void __launch_bounds__(kRowThreads) k_expert_combine_grad(const __gri
   constexpr int kN = Piece<DT>::kValues;
   constexpr uint64_t kSize = dtype_bytes(DT);
   __shared__ float part[kRowThreads / 32][kSlots];
-  pdl_trigger();
   pdl_wait();
   if (blockIdx.x >= a.tokens) {
     const uint64_t r0 = (blockIdx.x - a.tokens) * kFillRows;

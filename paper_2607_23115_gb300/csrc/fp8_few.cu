@@ -122,7 +122,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_few(const __grid_constant__
     for (uint32_t k = warp + lane * kWarps; k < kb; k += 32 * kWarps)
       prefetch(p + (uint64_t)k * kTileBytes, kRows * kTile);
   };
-  pdl_trigger();
   if (a.experts == 0) {
     // which weights is known: they come to L2, whatever the kernel before this one writes
     const uint32_t s0 = (uint32_t)((uint64_t)slabs * blockIdx.x / gridDim.x);

@@ -350,7 +350,6 @@ __device__ __forceinline__ void begin(Control& sh, const Counts& n, uint32_t col
   __syncthreads();
   if (cluster) cluster_sync();
   fence_after();
-  pdl_trigger();  // after the allocation: the next kernel's blocks come in behind it
 }
 
 // How many tiles there are, once the kernel before this one is done.

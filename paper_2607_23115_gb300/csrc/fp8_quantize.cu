@@ -87,7 +87,8 @@ __global__ void __launch_bounds__(kThreads, DT == GLEAM_FP32 ? 2 : 4) k_fp8_quan
   __shared__ uint32_t s_col[kThreads / 32][kTile];
   __shared__ __align__(16) uint8_t s_t[kTileBytes];
   pdl_wait();
-  pdl_trigger();  // in this order: a product chained to this kernel reads the weights before it waits
+  // in this order: the product that follows reads the weights before it waits
+  if (a.leads != 0) pdl_trigger();
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   uint64_t id = blockIdx.x;
   const uint64_t kb = id % a.kb;

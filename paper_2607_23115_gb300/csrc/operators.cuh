@@ -29,6 +29,7 @@ struct QuantizeArgs {
   uint32_t dtype, form;
   uint32_t vec;         // rows start 4-element aligned
   uint32_t fill;        // rows that are none are written as zeros
+  uint32_t leads;       // a product of the same call follows and may start early
   uint8_t *q, *qt;
   float *s, *st;
 };
@@ -210,7 +211,9 @@ struct Piece {
 };
 
 // Launches a kernel chained to the one before it on its stream: its blocks may
-// start while that one ends, and wait (pdl_wait) before they touch memory.
+// start while that one ends, and wait (pdl_wait) before they touch memory.  A kernel that ends
+// a public call does not let its dependents start early itself (pdl_trigger): what follows may
+// read its results without a wait, as an upload with GLEAM_OVERLAP_CALLS reads its payload.
 template <class... P>
 cudaError_t launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s,
                            uint32_t cluster, P... args) {

@@ -273,6 +273,7 @@ int gleam_fp8_linear(const gleam_fp8_linear_t* p, gleam_stream_t stream) {
   if (kb != 0) {
     QuantizeArgs q = quantize_args(x, p->d_src, p->per_token, p->rows, xq, xs);
     q.fill = E == 0 && p->d_src != nullptr;
+    q.leads = 1;
     GLEAM_TRY(cuda_err(launch_quantize(q, s)));
   }
   ProductArgs a{};
