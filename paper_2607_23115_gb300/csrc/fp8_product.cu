@@ -22,6 +22,8 @@
 // row of x, each one bulk copy in the order that the tensor cores read), warp 1, in the
 // wide kernel with warp 3, issues the products into two alternating parts of tensor memory,
 // warps 4 to 11 scale, add and store.
+#include <cuda.h>
+
 #include <algorithm>
 
 #include "operators.cuh"
@@ -43,7 +45,7 @@ __device__ __forceinline__ void mbar_init_n(uint32_t bar, uint32_t count) {
 // Barriers and state that both kernels keep in shared memory.
 struct Control {
   unsigned long long full[kMaxStages], empty[kMaxStages];    // stages of values
-  unsigned long long peer[kMaxStages];                       // the second block's stages (pairs)
+  unsigned long long peer[kMaxStages];                       // the second block's copies (pairs)
   unsigned long long tfull[2], tempty[2];                    // parts of tensor memory
   unsigned long long drain;
   unsigned long long pfull, pfree;  // partial sums: all here; read
@@ -227,14 +229,41 @@ __device__ __forceinline__ float4 peer_load(uint32_t addr) {
                : "memory");
   return v;
 }
-// An arrival that makes this thread's stores visible to the cluster, and one that only
-// says that tensor memory has been read or that copies have landed (the first waits for
-// every access that the thread has on its way: 900 cycles in an adding warp).
+// An arrival that makes what this thread wrote, and what it saw arrive, visible to the cluster,
+// and one that only says that tensor memory has been read: those reads are done
+// (tcgen05.wait::ld) and ordered by the tcgen05 fences before the arrival and after the wait for
+// it, for which PTX asks no more than a relaxed arrival (the first waits for every access
+// that the thread has on its way: 900 cycles in an adding warp).  Whoever waits for either does so
+// with the cluster as its scope (wait_phase<true>).
 __device__ __forceinline__ void peer_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void peer_signal(uint32_t bar) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// An arrival that only says how many bytes to expect.
+__device__ __forceinline__ void peer_expect_tx(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
+               : "memory");
+}
+
+// The tiles of an operand of a pair's product, as a tensor of three dimensions.  A copy of a tensor,
+// unlike one of bytes, may land in one block and arrive at the other's barrier, so that the first
+// block, which issues the products, waits for the second's copies themselves.  (Told of them
+// by a thread of the second, it takes a release in that thread, 1,100 cycles a stage: 8192 x 14336 x
+// 4096 took 546 us with one such thread, 460 with two.)
+template <bool kPair>
+struct Maps {};
+template <>
+struct Maps<true> {
+  CUtensorMap x, w;
+};
+__device__ __forceinline__ void copy_tile(uint32_t dst, const CUtensorMap* map, uint64_t tile, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], "
+      "[%1, {%2, %2, %3}], [%4];" ::"r"(dst),
+      "l"(map), "r"(0), "r"((uint32_t)tile), "r"(bar)
+      : "memory");
 }
 // Rows of expert e (or, over sums, its part of the contraction); none if they lie outside
 // the matrix.
@@ -321,7 +350,7 @@ __device__ __forceinline__ void begin(Control& sh, const Counts& n, uint32_t col
     for (uint32_t i = 0; i < n.stages; ++i) {
       mbar_init_n(smem_addr(&sh.full[i]), n.copiers);
       mbar_init_n(smem_addr(&sh.empty[i]), 1);
-      mbar_init_n(smem_addr(&sh.peer[i]), 1);
+      mbar_init_n(smem_addr(&sh.peer[i]), n.copiers);
     }
     for (uint32_t i = 0; i < 2; ++i) {
       mbar_init_n(smem_addr(&sh.tfull[i]), 1);
@@ -452,6 +481,7 @@ struct Wide {
     alignas(16) uint8_t out[kAdders][32 * kOutPitch];
     alignas(16) float xscales[kPlaces][kTile];
     alignas(16) float wscales[kPlaces][NT];  // with a scale for each row of w
+    unsigned long long scaled[kPlaces];  // pairs: a place's scales are here
     Control c;
   };
   static constexpr uint32_t kBytes = 1024 + kStages * kStage + sizeof(Shared);
@@ -546,7 +576,8 @@ __device__ __forceinline__ void store_rows(const ProductArgs& a, const unsigned 
 }
 
 template <int NT, bool kBlocks, bool kPair>
-__global__ void __launch_bounds__(kThreads, 1) k_fp8_wide(const __grid_constant__ ProductArgs a) {
+__global__ void __launch_bounds__(kThreads, 1)
+    k_fp8_wide(const __grid_constant__ ProductArgs a, const __grid_constant__ Maps<kPair> maps) {
   using W = Wide<NT, kPair>;
   constexpr uint32_t kStages = W::kStages, kStage = W::kStage;
   constexpr int kCols = W::kCols;
@@ -560,6 +591,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_wide(const __grid_constant_
   const uint32_t rank = kPair ? cluster_rank() : 0;
   const uint32_t id0 = blockIdx.x / kBlocksOfTile, ids = gridDim.x / kBlocksOfTile;
 
+  if (kPair && threadIdx.x == 0)
+    for (uint32_t i = 0; i < W::kPlaces; ++i) mbar_init_n(smem_addr(&ws.scaled[i]), kBlocks ? 1 : 2);
   begin<kPair>(sh, Counts{kStages, 2, kBlocksOfTile * kAdders, 1}, 2 * NT, kPair);
   pdl_wait();
   count_tiles<W::kRows, NT>(a, sh);
@@ -581,33 +614,51 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_wide(const __grid_constant_
         const uint32_t xbytes = ((own_rows(t) + 7) & ~7u) * kTile;
         const uint64_t wrow = t.w0 / kTile + rank;  // row tiles of w that exist, of this block's
         const uint32_t wtiles = wrow < a.wrt ? (uint32_t)min((uint64_t)(W::kOwnW / kTile), a.wrt - wrow) : 0;
-        const uint8_t* xq = a.xq + (t.x0 / kTile + rank) * a.kb * kTileBytes;
-        const uint8_t* wq = a.wq + (t.wtile + rank) * a.kb * kTileBytes;
         // rows of w that the tile has, for their scales
         const uint32_t wscales = (uint32_t)min((uint64_t)NT, (a.wrt - t.w0 / kTile) * kTile) * 4;
-        const uint32_t bytes = warp == 0 ? xbytes + (xbytes != 0 ? kTile * 4 : 0)
-                                         : wtiles * kTileBytes + (kBlocks ? 0 : wscales);
+        const uint64_t xtile = (t.x0 / kTile + rank) * a.kb, wtile = (t.wtile + rank) * a.kb;
+        const uint32_t values = warp == 0 ? (kPair && xbytes != 0 ? kTileBytes : xbytes) : wtiles * kTileBytes;
+        const uint32_t scales = warp == 0 ? (xbytes != 0 ? kTile * 4 : 0) : (kBlocks ? 0 : wscales);
         for (uint32_t kb = t.kb0; kb < t.kb1; ++kb) {
-          if (!(ok = wait_phase(smem_addr(&sh.empty[st.i]), st.phase ^ 1, sh, a.status))) break;
-          const uint32_t bar = smem_addr(&sh.full[st.i]);
+          if (!(ok = wait_phase<kPair>(smem_addr(&sh.empty[st.i]), st.phase ^ 1, sh, a.status))) break;
           const uint32_t dst = smem_addr(base + st.i * kStage);
-          mbar_expect_tx(bar, bytes);
+          uint32_t bar = smem_addr(&sh.full[st.i]), scaled = bar;
+          if constexpr (kPair) {
+            if (rank == 0) {
+              mbar_expect_tx(bar, values);
+            } else {
+              bar = peer_addr(smem_addr(&sh.peer[st.i]), 0);
+              peer_expect_tx(bar, values);
+            }
+            scaled = smem_addr(&ws.scaled[place]);
+            if (warp == 0 || !kBlocks) mbar_expect_tx(scaled, scales);
+          } else {
+            mbar_expect_tx(bar, values + scales);
+          }
           if (warp == 0) {
             if (xbytes != 0) {
-              copy_in(dst, xq + (uint64_t)kb * kTileBytes, xbytes, bar);
-              copy_in(smem_addr(ws.xscales[place]), a.xs + kb * (a.xrt * kTile) + t.x0 + rank * kTile, kTile * 4, bar);
+              if constexpr (kPair) copy_tile(dst, &maps.x, xtile + kb, bar);
+              else copy_in(dst, a.xq + (xtile + kb) * kTileBytes, xbytes, bar);
+              copy_in(smem_addr(ws.xscales[place]), a.xs + kb * (a.xrt * kTile) + t.x0 + rank * kTile, scales, scaled);
             }
           } else {
-            for (uint32_t i = 0; i < wtiles; ++i)
-              copy_in(dst + (1 + i) * kTileBytes, wq + (i * a.kb + kb) * kTileBytes, kTileBytes, bar);
+            for (uint32_t i = 0; i < wtiles; ++i) {
+              const uint32_t to = dst + (1 + i) * kTileBytes;
+              if constexpr (kPair) copy_tile(to, &maps.w, wtile + kb, bar);
+              else copy_in(to, a.wq + (wtile + i * a.kb + kb) * kTileBytes, kTileBytes, bar);
+            }
             if (!kBlocks)
-              copy_in(smem_addr(ws.wscales[place]), a.ws + kb * (a.wrt * kTile) + t.w0, wscales, bar);
+              copy_in(smem_addr(ws.wscales[place]), a.ws + kb * (a.wrt * kTile) + t.w0, scales, scaled);
           }
           st.next(kStages);
           if (++place == W::kPlaces) place = 0;
         }
       }
-      if (!ok) await_copies(sh, st, kStages);
+      // the other block's arrivals for the last stages land before this block's memory goes to another
+      if (kPair)
+        for (uint32_t i = 0; ok && i < kStages; ++i, st.next(kStages))
+          ok = wait_phase<true>(smem_addr(&sh.empty[st.i]), st.phase ^ 1, sh, a.status);
+      if (!ok && rank == 0) await_copies(sh, st, kStages);
     } else if (rank == 0 && (warp == 1 || (W::kTurns && warp == 3)) && lane == 0) {
       // products: in turns, one thread's waits pass while the other's products run (a thread
       // stands still while it issues)
@@ -618,8 +669,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_wide(const __grid_constant_
         for (uint32_t kb = t.kb0; kb < t.kb1; ++kb) {
           if (!W::kTurns || tm.i == warp / 2) {
             if (!(ok = wait_phase(smem_addr(&sh.full[st.i]), st.phase, sh, a.status))) break;
-            if (kPair && !(ok = wait_phase(smem_addr(&sh.peer[st.i]), st.phase, sh, a.status))) break;
-            if (!(ok = wait_phase(smem_addr(&sh.tempty[tm.i]), tm.phase ^ 1, sh, a.status))) break;
+            if (kPair && !(ok = wait_phase<true>(smem_addr(&sh.peer[st.i]), st.phase, sh, a.status))) break;
+            if (!(ok = wait_phase<kPair>(smem_addr(&sh.tempty[tm.i]), tm.phase ^ 1, sh, a.status))) break;
             fence_after();
             const uint32_t at = smem_addr(base + st.i * kStage);
             issue_block<NT, kPair>(tmem + tm.i * NT, at, at + kTileBytes);
@@ -631,18 +682,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_wide(const __grid_constant_
         }
       }
       if (!ok) await_products<kPair>(sh);
-    } else if (kPair && rank == 1 && warp == 1 && lane == 0) {
-      // the second block's stages are complete: the first block issues
-      Ring st;
-      bool ok = true;
-      for (uint32_t id = id0; ok && id < total; id += ids) {
-        const Tile t = decode<W::kRows, NT>(a, sh, id);
-        for (uint32_t kb = t.kb0; kb < t.kb1; ++kb) {
-          if (!(ok = wait_phase(smem_addr(&sh.full[st.i]), st.phase, sh, a.status))) break;
-          peer_signal(peer_addr(smem_addr(&sh.peer[st.i]), 0));
-          st.next(kStages);
-        }
-      }
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
@@ -650,8 +689,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_wide(const __grid_constant_
     const uint32_t taddr = tmem + ((warp % 4) * 32 << 16) + half * kCols;
     // part 0 of tensor memory is free once both blocks' adding warps say so to the first
     const uint32_t tempty = kPair ? peer_addr(smem_addr(&sh.tempty[0]), 0) : smem_addr(&sh.tempty[0]);
-    Ring tm;
-    uint32_t place = 0;
+    Ring tm, at;  // at: the block's scales
     bool ok = true;
     for (uint32_t id = id0; ok && id < total; id += ids) {
       const Tile t = decode<W::kRows, NT>(a, sh, id);
@@ -665,7 +703,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_wide(const __grid_constant_
       float sw32 = 0;
       for (uint32_t kb = t.kb0; kb < t.kb1; ++kb) {
         if (kBlocks && (kb - t.kb0) % 32 == 0) sw32 = __ldg(wsp + min(kb + lane, t.kb1 - 1));
-        ok = __all_sync(0xffffffffu, wait_phase(smem_addr(&sh.tfull[tm.i]), tm.phase, sh, a.status));
+        ok = __all_sync(0xffffffffu, (!kPair || wait_phase(smem_addr(&ws.scaled[at.i]), at.phase, sh, a.status)) &&
+                                         wait_phase<kPair>(smem_addr(&sh.tfull[tm.i]), tm.phase, sh, a.status));
         if (!ok) break;
         fence_after();
         const uint32_t part = taddr + tm.i * NT;
@@ -673,7 +712,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_wide(const __grid_constant_
         // registers, the next products may come
         float v[2][kLoad];
         if constexpr (kBlocks) {
-          const float f = ws.xscales[place][row] * __shfl_sync(0xffffffffu, sw32, (kb - t.kb0) % 32);
+          const float f = ws.xscales[at.i][row] * __shfl_sync(0xffffffffu, sw32, (kb - t.kb0) % 32);
           const unsigned long long f2 = pair(f, f);
           tmem_load(part, v[0]);
 #pragma unroll
@@ -699,10 +738,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_wide(const __grid_constant_
           unsigned long long f2[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float f = ws.xscales[place][(warp % 4) * 32 + lane / 4 + 8 * j];
+            const float f = ws.xscales[at.i][(warp % 4) * 32 + lane / 4 + 8 * j];
             f2[j] = pair(f, f);
           }
-          const float* s = ws.wscales[place] + half * kCols + 2 * (lane % 4);
+          const float* s = ws.wscales[at.i] + half * kCols + 2 * (lane % 4);
           tmem_load_pieces(part, v[0]);
 #pragma unroll
           for (int c = 0; c < kCols; c += kLoad) {
@@ -730,16 +769,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_wide(const __grid_constant_
           }
         }
         tm.next(2);
-        if (++place == W::kPlaces) place = 0;
+        at.next(W::kPlaces);
       }
       if (!ok) break;
       const uint32_t quarter = (warp % 4) * 32;
       const uint32_t rows = own_rows(t) > quarter ? own_rows(t) - quarter : 0;
-      const uint64_t at = t.y + (t.x0 + rank * kTile + quarter) * a.ld, col = t.w0 + half * kCols;
+      const uint64_t first = t.y + (t.x0 + rank * kTile + quarter) * a.ld, col = t.w0 + half * kCols;
       uint8_t* out = ws.out[warp - 4];
-      if (a.dtype == GLEAM_BF16) store_rows<GLEAM_BF16, kCols, !kBlocks>(a, acc, at, col, rows, lane, out);
-      else if (a.dtype == GLEAM_FP16) store_rows<GLEAM_FP16, kCols, !kBlocks>(a, acc, at, col, rows, lane, out);
-      else store_rows<GLEAM_FP32, kCols, !kBlocks>(a, acc, at, col, rows, lane, out);
+      if (a.dtype == GLEAM_BF16) store_rows<GLEAM_BF16, kCols, !kBlocks>(a, acc, first, col, rows, lane, out);
+      else if (a.dtype == GLEAM_FP16) store_rows<GLEAM_FP16, kCols, !kBlocks>(a, acc, first, col, rows, lane, out);
+      else store_rows<GLEAM_FP32, kCols, !kBlocks>(a, acc, first, col, rows, lane, out);
     }
   }
   finish<kPair>(tmem, 2 * NT, kPair);
@@ -1000,11 +1039,42 @@ struct Gpu {
   }
 };
 
-template <class K>
-cudaError_t start(K kernel, uint32_t bytes, const ProductArgs& a, uint64_t blocks, uint32_t cluster, cudaStream_t s) {
+template <class... P>
+cudaError_t start(void (*kernel)(ProductArgs, P...), uint32_t bytes, const ProductArgs& a, uint64_t blocks,
+                  uint32_t cluster, cudaStream_t s, P... more) {
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
   if (e != cudaSuccess) return e;
-  return launch_chained(kernel, dim3((unsigned)blocks), dim3(kThreads), bytes, s, cluster, a);
+  return launch_chained(kernel, dim3((unsigned)blocks), dim3(kThreads), bytes, s, cluster, a, more...);
+}
+
+typedef decltype(&cuTensorMapEncodeTiled) EncodeFn;
+
+// The driver's function that describes a tensor to the copies; it needs no GPU work.
+EncodeFn encode_fn() {
+  static const EncodeFn fn = []() -> EncodeFn {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      return nullptr;
+    }
+    return reinterpret_cast<EncodeFn>(f);
+  }();
+  return fn;
+}
+
+// `tiles` tiles of 128 x 128 bytes, one after the other; a copy takes one.
+cudaError_t map_tiles(CUtensorMap* map, const uint8_t* q, uint64_t tiles) {
+  const EncodeFn fn = encode_fn();
+  if (fn == nullptr) return cudaErrorNotSupported;
+  if (tiles > 0x7fffffffull) return cudaErrorInvalidValue;
+  const cuuint64_t dims[3] = {kTile, kTile, tiles}, strides[2] = {kTile, kTileBytes};
+  const cuuint32_t box[3] = {kTile, kTile, 1}, step[3] = {1, 1, 1};
+  const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<uint8_t*>(q), dims, strides, box, step,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
 // Tiles of kX rows of x by kW of w (over rows: at most, as the offsets are on the device).
@@ -1022,8 +1092,17 @@ cudaError_t wide(ProductArgs a, int sms, cudaStream_t s) {
   a.tiles = tiles_of(a, W::kRows, NT);
   if (a.tiles >= 0x7fffffffull) return cudaErrorInvalidValue;
   const uint64_t blocks = per * std::min<uint64_t>(a.tiles, (uint64_t)sms / per);
+  Maps<kPair> maps{};
+  if constexpr (kPair) {
+    const uint64_t weights = a.experts != 0 && a.over == GLEAM_OVER_ROWS ? a.experts : 1;
+    cudaError_t e = cudaSuccess;
+    // without a contraction nothing is copied
+    if (a.kb != 0 && ((e = map_tiles(&maps.x, a.xq, a.xrt * a.kb)) != cudaSuccess ||
+                      (e = map_tiles(&maps.w, a.wq, weights * a.wrt * a.kb)) != cudaSuccess))
+      return e;
+  }
   return start(a.w_form == GLEAM_FP8_BLOCKS ? k_fp8_wide<NT, true, kPair> : k_fp8_wide<NT, false, kPair>, W::kBytes,
-               a, blocks, per, s);
+               a, blocks, per, s, maps);
 }
 
 // The contraction is shared out among 1, 2, 4 or 8 blocks, as many as keep the GPU's SMs

@@ -83,8 +83,8 @@ def test_quantised_weights(n, k, chunk, linear):
     assert [r[0][1] for r in calls[:3]] == [like.q.numel() // chunk, 1, 1]
 
 
-# rows of x: one kernel; w's rows as the lanes; x's
-@pytest.mark.parametrize("m,n,k", [(3, 4096, 512), (40, 4096, 512), (300, 4096, 512)])
+# rows of x: one kernel; w's rows as the lanes; x's, by one block and by two
+@pytest.mark.parametrize("m,n,k", [(3, 4096, 512), (40, 4096, 512), (300, 4096, 512), (4096, 4096, 512)])
 def test_products(m, n, k):
     xs = [torch.randn(m, k, device=DEV).to(torch.bfloat16) for _ in range(5)]
     w = fp8.quantize_weight(0.02 * torch.randn(n, k, device=DEV))
