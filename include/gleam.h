@@ -529,6 +529,12 @@ uint64_t gleam_fp8_linear_work(uint64_t rows, uint64_t cols, uint32_t experts);
  * once the call's work is done. */
 int gleam_fp8_linear(const gleam_fp8_linear_t* p, gleam_stream_t stream);
 
+/* Test hooks of the products, for the whole process.  what = GLEAM_DEBUG_WAIT_LIMIT_NS: limit of
+ * the waits on the device in nanoseconds (default 4e9).  what = GLEAM_DEBUG_SKIP_ARRIVE: in
+ * the next product, the first block's first copying thread stops after `value` copies, so that
+ * waits run out. */
+int gleam_operators_debug_set(int what, int64_t value);
+
 /* ---- tokens by expert -----------------------------------------------------
  * A router gives each of `tokens` tokens `per_token` experts: slot
  * i = t * per_token + j goes to expert d_ids[i] (id_bytes 4 or 8; an id outside

@@ -35,12 +35,12 @@ __device__ __forceinline__ void mma_e4m3(float (&c)[4], uint32_t a0, uint32_t a1
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Waits for a phase for at most kOperatorWaitNs.  The clock answers late, so it is asked after some looks.
-__device__ __forceinline__ bool arrived(uint32_t bar, uint32_t parity) {
+// Waits for a phase for at most limit_ns.  The clock answers late, so it is asked after some looks.
+__device__ __forceinline__ bool arrived(uint32_t bar, uint32_t parity, unsigned long long limit_ns) {
 #pragma unroll 1
   for (int i = 0; i < 64; ++i)
     if (mbar_try_wait(bar, parity)) return true;
-  return mbar_wait(bar, parity, kOperatorWaitNs);
+  return mbar_wait(bar, parity, limit_ns);
 }
 
 // A lane's two pieces of a block: 16 values from column `col` and 16 from `col` + 64, as loaded.
@@ -111,7 +111,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_few(const __grid_constant__
   const uint32_t bars = (uint32_t)__cvta_generic_to_shared(&sh.full[warp][0]);
   uint32_t stage = 0, phase = 0;       // read next
   uint32_t to_stage = 0;                // filled next
-  bool ok = true;
+  uint64_t asked = 0;                   // chunks so far
+  bool ok = true;                       // no wait has run out: once one has, no chunk is asked for
+  const uint32_t most = blockIdx.x == 0 && warp == 0 ? a.skip : kNoSkip;
   if (lane == 0) {
     for (uint32_t i = 0; i < a.stages; ++i) mbar_init(bars + 8 * i);
     mbar_fence_init();
@@ -188,7 +190,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_few(const __grid_constant__
       // Chunks: the warp's blocks of a slab, slab after slab, a.stages of them on their way.
       uint32_t lslab = slab0, lk = warp;  // asked for next
       auto ask = [&]() {
-        if (lane == 0 && lslab < slab1 && lk < kb) {
+        if (lane == 0 && ok && lslab < slab1 && lk < kb && (most == kNoSkip || asked < most)) {
+          ++asked;
           const uint32_t wt = lslab * kRows / kTile;
           mbar_expect_tx(bars + 8 * to_stage, kChunk);
           copy_in((uint32_t)__cvta_generic_to_shared(ring + to_stage * kChunk),
@@ -262,7 +265,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_few(const __grid_constant__
         float acc[kGroups][4] = {};
         for (uint32_t k = warp; k < kb; k += kWarps) {
           const float sw = __ldg(wsp + k);
-          if (lane == 0 && ok) ok = arrived(bars + 8 * stage, phase);
+          if (lane == 0 && ok) ok = arrived(bars + 8 * stage, phase, a.wait_ns);
           __syncwarp();
           const uint8_t* c0 = ring + stage * kChunk;
           const uint4 w0 = *reinterpret_cast<const uint4*>(c0 + p0), w1 = *reinterpret_cast<const uint4*>(c0 + p1);
@@ -316,10 +319,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_few(const __grid_constant__
       __syncwarp();  // this warp's blocks of x have been read
     }
   }
-  // a wait ran out: what it waited for comes before this block's memory goes to another
+  // a wait ran out: chunks on their way land before this block's memory goes to another
   if (lane == 0 && !ok) {
     if (a.status != nullptr) *a.status = GLEAM_ERR_TIMEOUT;
-    for (uint32_t i = 0; i < a.stages; ++i) mbar_wait(bars + 8 * i, phase ^ (i < stage), kOperatorWaitNs);
+    settle_ring(&asked, 1, a.stages, [](uint32_t) {},
+                [&](uint32_t i, uint32_t parity) { mbar_wait(bars + 8 * i, parity, kOperatorWaitNs); });
   }
 }
 

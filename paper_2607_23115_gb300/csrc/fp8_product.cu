@@ -88,17 +88,6 @@ __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, Contro
   }
 }
 
-// A position in a ring of n barriers.
-struct Ring {
-  uint32_t i = 0, phase = 0;
-  __device__ __forceinline__ void next(uint32_t n) {
-    if (++i == n) {
-      i = 0;
-      phase ^= 1;
-    }
-  }
-};
-
 // Shared memory descriptor of rows of 128 bytes, swizzled over 128 bytes, contraction along
 // the row: 8 rows are 1024 bytes apart from the next 8.
 __device__ __forceinline__ uint64_t tile_descriptor(uint32_t addr) {

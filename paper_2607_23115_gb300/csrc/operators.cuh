@@ -8,14 +8,17 @@
 #include <cstdint>
 
 #include "gleam_internal.cuh"
+#include "ring.cuh"
 
 namespace gleam {
 
 constexpr uint32_t kTile = 128;                // rows and columns of a tile, values of a group
 constexpr uint32_t kTileBytes = kTile * kTile;  // e4m3
 constexpr uint32_t kMaxExperts = 1024;
-// Limit of a wait inside the product kernel.
+// Limit of a wait inside the product kernels (gleam_operators_debug_set may lower it), and of a
+// wait for copies and products in flight once another has run out.
 constexpr unsigned long long kOperatorWaitNs = 4000000000ULL;
+constexpr uint32_t kNoSkip = 0xffffffffu;
 
 struct QuantizeArgs {
   const uint8_t* x;
@@ -69,6 +72,8 @@ struct FewArgs {
   uint32_t experts;
   const int32_t *offsets, *counts;
   int32_t* status;
+  unsigned long long wait_ns;
+  uint32_t skip;          // test hook: block 0 asks for no chunk after so many (kNoSkip: none)
 };
 
 struct SortArgs {

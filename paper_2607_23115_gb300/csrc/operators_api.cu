@@ -1,5 +1,7 @@
 // C entry points of the operators on 8-bit weights and on tokens sorted by expert
 // (include/gleam.h): argument checks, then one launch each.
+#include <atomic>
+
 #include "host_checks.cuh"
 #include "operators.cuh"
 
@@ -76,6 +78,14 @@ uint64_t rows_to_expect(uint64_t rows, uint32_t experts) {
 bool one_kernel(uint64_t rows, uint64_t cols, uint32_t experts) {
   return rows_to_expect(rows, experts) <= (experts == 0 ? kFewRows : kFewRowsOfExpert) &&
          few_fits(experts == 0 ? rows : 1, tiles_of(cols));
+}
+
+// Test hooks (gleam_operators_debug_set).
+std::atomic<unsigned long long> g_wait_ns{kOperatorWaitNs};
+std::atomic<uint32_t> g_skip{kNoSkip};
+// It applies to one call.
+uint32_t take_skip() {
+  return g_skip.load(std::memory_order_relaxed) == kNoSkip ? kNoSkip : g_skip.exchange(kNoSkip);
 }
 
 #define GLEAM_TRY(x)              \
@@ -266,6 +276,8 @@ int gleam_fp8_linear(const gleam_fp8_linear_t* p, gleam_stream_t stream) {
     f.offsets = p->ex.d_offsets;
     f.counts = p->ex.d_counts;
     f.status = p->d_status;
+    f.wait_ns = g_wait_ns.load(std::memory_order_relaxed);
+    f.skip = take_skip();
     return cuda_err(launch_few(f, s));
   }
   uint8_t* xq = static_cast<uint8_t*>(p->d_work);
@@ -299,6 +311,19 @@ int gleam_fp8_linear(const gleam_fp8_linear_t* p, gleam_stream_t stream) {
   a.counts = p->ex.d_counts;
   a.status = p->d_status;
   return cuda_err(launch_product(a, rows_to_expect(p->rows, E), s));
+}
+
+int gleam_operators_debug_set(int what, int64_t value) {
+  if (value <= 0) return GLEAM_ERR_INVALID_ARG;
+  if (what == GLEAM_DEBUG_WAIT_LIMIT_NS) {
+    g_wait_ns = (unsigned long long)value;
+    return GLEAM_OK;
+  }
+  if (what == GLEAM_DEBUG_SKIP_ARRIVE && value < (int64_t)kNoSkip) {
+    g_skip = (uint32_t)value;
+    return GLEAM_OK;
+  }
+  return GLEAM_ERR_INVALID_ARG;
 }
 
 uint64_t gleam_expert_rows(uint64_t tokens, uint32_t per_token, uint32_t experts, uint32_t align) {
