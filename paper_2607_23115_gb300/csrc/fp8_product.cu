@@ -47,10 +47,11 @@ struct Control {
   unsigned long long full[kMaxStages], empty[kMaxStages];    // stages of values
   unsigned long long peer[kMaxStages];                       // the second block's copies (pairs)
   unsigned long long tfull[2], tempty[2];                    // parts of tensor memory
-  unsigned long long drain;
+  unsigned long long drain[2];       // an issuing thread's products, once a wait has run out
+  uint64_t filled[2];                // stages that each copying thread has filled
   unsigned long long pfull, pfree;  // partial sums: all here; read
   uint32_t tmem;
-  uint32_t dead;                    // a wait ran out
+  uint32_t dead;                    // a wait ran out (in the end: of any block of the cluster)
   uint32_t total;                   // tiles
   uint32_t first[kMaxExperts];      // an expert's first tile (over rows)
 };
@@ -68,10 +69,10 @@ __device__ __forceinline__ bool try_phase(uint32_t bar, uint32_t parity) {
       : "memory");
   return done != 0;
 }
-// Waits for a phase, at most kOperatorWaitNs; false once any wait of the block ran out.  The
+// Waits for a phase, at most a.wait_ns; false once any wait of the block ran out.  The
 // clock is read only once a while: it answers late.
 template <bool kPeers = false>
-__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, Control& sh, int32_t* status) {
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, Control& sh, const ProductArgs& a) {
   if (try_phase<kPeers>(bar, parity)) return true;
   unsigned long long t0 = 0;
   for (uint32_t i = 1;; ++i) {
@@ -80,9 +81,9 @@ __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, Contro
     if (*reinterpret_cast<volatile uint32_t*>(&sh.dead)) return false;
     const unsigned long long now = globaltimer_ns();
     if (t0 == 0) t0 = now;
-    if (now - t0 > kOperatorWaitNs) {
+    if (now - t0 > a.wait_ns) {
       *reinterpret_cast<volatile uint32_t*>(&sh.dead) = 1;
-      if (status != nullptr) *status = GLEAM_ERR_TIMEOUT;
+      if (a.status != nullptr) *a.status = GLEAM_ERR_TIMEOUT;
       return false;
     }
   }
@@ -218,6 +219,14 @@ __device__ __forceinline__ float4 peer_load(uint32_t addr) {
                : "memory");
   return v;
 }
+__device__ __forceinline__ void peer_store(uint32_t addr, uint32_t v) {
+  asm volatile("st.relaxed.cluster.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+__device__ __forceinline__ uint64_t peer_load64(uint32_t addr) {
+  uint64_t v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
+  return v;
+}
 // An arrival that makes what this thread wrote, and what it saw arrive, visible to the cluster,
 // and one that only says that tensor memory has been read: those reads are done
 // (tcgen05.wait::ld) and ordered by the tcgen05 fences before the arrival and after the wait for
@@ -345,7 +354,10 @@ __device__ __forceinline__ void begin(Control& sh, const Counts& n, uint32_t col
       mbar_init_n(smem_addr(&sh.tfull[i]), 1);
       mbar_init_n(smem_addr(&sh.tempty[i]), n.adders);
     }
-    mbar_init_n(smem_addr(&sh.drain), 1);
+    for (uint32_t i = 0; i < 2; ++i) {
+      mbar_init_n(smem_addr(&sh.drain[i]), 1);
+      sh.filled[i] = 0;
+    }
     mbar_init_n(smem_addr(&sh.pfull), n.partials);
     mbar_init_n(smem_addr(&sh.pfree), n.partials);
     sh.dead = 0;
@@ -403,14 +415,28 @@ __device__ __forceinline__ void count_tiles(const ProductArgs& a, Control& sh) {
   __syncthreads();
 }
 
-// In a cluster, no block leaves while another may still write to it or read its memory.
-template <bool kPair>
-__device__ __forceinline__ void finish(uint32_t tmem, uint32_t columns, bool cluster) {
+// In a cluster, no block leaves while another may still write to it or read its memory.  Once a
+// wait has run out, settle waits for all copies and products on their way, whichever threads asked
+// for them, before memory and tensor memory go to another block.
+template <bool kPair, class Settle>
+__device__ __forceinline__ void finish(const Control& sh, uint32_t tmem, uint32_t columns, bool cluster,
+                                       Settle settle) {
   __syncwarp();
   fence_before();
   __syncthreads();
-  if (cluster) cluster_sync();
+  const volatile uint32_t* dead = &sh.dead;
+  if (cluster) {
+    if (threadIdx.x < cluster_size() && *dead) peer_store(peer_addr(smem_addr(&sh.dead), threadIdx.x), 1);
+    __syncwarp();
+    cluster_sync();
+  }
   fence_after();
+  if (*dead) {
+    settle();
+    __syncwarp();
+    __syncthreads();
+    if (cluster) cluster_sync();
+  }
   if (threadIdx.x / 32 == 1) {
     if constexpr (kPair)
       asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns));
@@ -420,15 +446,18 @@ __device__ __forceinline__ void finish(uint32_t tmem, uint32_t columns, bool clu
   if (kPair) cluster_sync();
 }
 
-// Copies in flight when a wait ran out land before the block's memory goes to another.
-__device__ __forceinline__ void await_copies(Control& sh, const Ring& st, uint32_t n) {
-  for (uint32_t i = 0; i < n; ++i)
-    mbar_wait(smem_addr(&sh.full[i]), st.phase ^ (i >= st.i), kOperatorWaitNs);
-}
+// Products that this thread, the i-th that issues any, has asked for are done (in both blocks of a
+// pair, of which the first issues).
 template <bool kPair>
-__device__ __forceinline__ void await_products(Control& sh) {
-  mma_commit<kPair>(smem_addr(&sh.drain));
-  mbar_wait(smem_addr(&sh.drain), 0, kOperatorWaitNs);
+__device__ __forceinline__ void await_products(Control& sh, uint32_t i, bool issues) {
+  if (issues) mma_commit<kPair>(smem_addr(&sh.drain[i]));
+  mbar_wait(smem_addr(&sh.drain[i]), 0, kOperatorWaitNs);
+}
+// Copies on their way to a ring of n stages have landed.
+__device__ __forceinline__ void await_copies(const uint64_t* filled, uint32_t threads, unsigned long long* bars,
+                                             uint32_t n) {
+  settle_ring(filled, threads, n, [&](uint32_t i) { mbar_arrive(smem_addr(&bars[i])); },
+              [&](uint32_t i, uint32_t parity) { mbar_wait(smem_addr(&bars[i]), parity, kOperatorWaitNs); });
 }
 
 // One block of the contraction: 128 lanes (of each block) from `a`, NT columns from `b`.
@@ -597,6 +626,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       // copies: warp 0 those of x, warp 2 those of w
       Ring st;
       uint32_t place = 0;
+      uint64_t filled = 0;
+      const uint64_t most = blockIdx.x == 0 && warp == 0 && a.skip != kNoSkip ? a.skip : ~0ull;
       bool ok = true;
       for (uint32_t id = id0; ok && id < total; id += ids) {
         const Tile t = decode<W::kRows, NT>(a, sh, id);
@@ -609,7 +640,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t values = warp == 0 ? (kPair && xbytes != 0 ? kTileBytes : xbytes) : wtiles * kTileBytes;
         const uint32_t scales = warp == 0 ? (xbytes != 0 ? kTile * 4 : 0) : (kBlocks ? 0 : wscales);
         for (uint32_t kb = t.kb0; kb < t.kb1; ++kb) {
-          if (!(ok = wait_phase<kPair>(smem_addr(&sh.empty[st.i]), st.phase ^ 1, sh, a.status))) break;
+          if (!(ok = filled < most && wait_phase<kPair>(smem_addr(&sh.empty[st.i]), st.phase ^ 1, sh, a))) break;
+          ++filled;
           const uint32_t dst = smem_addr(base + st.i * kStage);
           uint32_t bar = smem_addr(&sh.full[st.i]), scaled = bar;
           if constexpr (kPair) {
@@ -646,8 +678,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       // the other block's arrivals for the last stages land before this block's memory goes to another
       if (kPair)
         for (uint32_t i = 0; ok && i < kStages; ++i, st.next(kStages))
-          ok = wait_phase<true>(smem_addr(&sh.empty[st.i]), st.phase ^ 1, sh, a.status);
-      if (!ok && rank == 0) await_copies(sh, st, kStages);
+          ok = wait_phase<true>(smem_addr(&sh.empty[st.i]), st.phase ^ 1, sh, a);
+      sh.filled[warp / 2] = filled;
     } else if (rank == 0 && (warp == 1 || (W::kTurns && warp == 3)) && lane == 0) {
       // products: in turns, one thread's waits pass while the other's products run (a thread
       // stands still while it issues)
@@ -657,9 +689,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         const Tile t = decode<W::kRows, NT>(a, sh, id);
         for (uint32_t kb = t.kb0; kb < t.kb1; ++kb) {
           if (!W::kTurns || tm.i == warp / 2) {
-            if (!(ok = wait_phase(smem_addr(&sh.full[st.i]), st.phase, sh, a.status))) break;
-            if (kPair && !(ok = wait_phase<true>(smem_addr(&sh.peer[st.i]), st.phase, sh, a.status))) break;
-            if (!(ok = wait_phase<kPair>(smem_addr(&sh.tempty[tm.i]), tm.phase ^ 1, sh, a.status))) break;
+            if (!(ok = wait_phase(smem_addr(&sh.full[st.i]), st.phase, sh, a))) break;
+            if (kPair && !(ok = wait_phase<true>(smem_addr(&sh.peer[st.i]), st.phase, sh, a))) break;
+            if (!(ok = wait_phase<kPair>(smem_addr(&sh.tempty[tm.i]), tm.phase ^ 1, sh, a))) break;
             fence_after();
             const uint32_t at = smem_addr(base + st.i * kStage);
             issue_block<NT, kPair>(tmem + tm.i * NT, at, at + kTileBytes);
@@ -670,7 +702,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           tm.next(2);
         }
       }
-      if (!ok) await_products<kPair>(sh);
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
@@ -692,8 +723,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       float sw32 = 0;
       for (uint32_t kb = t.kb0; kb < t.kb1; ++kb) {
         if (kBlocks && (kb - t.kb0) % 32 == 0) sw32 = __ldg(wsp + min(kb + lane, t.kb1 - 1));
-        ok = __all_sync(0xffffffffu, (!kPair || wait_phase(smem_addr(&ws.scaled[at.i]), at.phase, sh, a.status)) &&
-                                         wait_phase<kPair>(smem_addr(&sh.tfull[tm.i]), tm.phase, sh, a.status));
+        ok = __all_sync(0xffffffffu, (!kPair || wait_phase(smem_addr(&ws.scaled[at.i]), at.phase, sh, a)) &&
+                                         wait_phase<kPair>(smem_addr(&sh.tfull[tm.i]), tm.phase, sh, a));
         if (!ok) break;
         fence_after();
         const uint32_t part = taddr + tm.i * NT;
@@ -770,7 +801,19 @@ __global__ void __launch_bounds__(kThreads, 1)
       else store_rows<GLEAM_FP32, kCols, !kBlocks>(a, acc, first, col, rows, lane, out);
     }
   }
-  finish<kPair>(tmem, 2 * NT, kPair);
+  finish<kPair>(sh, tmem, 2 * NT, kPair, [&] {
+    if ((warp == 1 || (W::kTurns && warp == 3)) && lane == 0) await_products<kPair>(sh, warp / 2, rank == 0);
+    if (threadIdx.x != 0) return;
+    if (rank == 0) await_copies(sh.filled, 2, sh.full, kStages);
+    if constexpr (kPair) {
+      if (rank == 0) {
+        const uint64_t theirs[2] = {peer_load64(peer_addr(smem_addr(&sh.filled[0]), 1)),
+                                    peer_load64(peer_addr(smem_addr(&sh.filled[1]), 1))};
+        await_copies(theirs, 2, sh.peer, kStages);
+      }
+      await_copies(sh.filled, kBlocks ? 1 : 2, ws.scaled, W::kPlaces);
+    }
+  });
 }
 
 // ---- narrow ----------------------------------------------------------------
@@ -877,6 +920,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_narrow(const __grid_constan
     // copies: warp 0 those of w, warp 2 those of x and its scales
     Ring st;
     uint32_t place = 0;
+    uint64_t filled = ahead;
+    const uint64_t most = blockIdx.x == 0 && warp == 0 && a.skip != kNoSkip ? a.skip : ~0ull;
     bool ok = true;
     for (uint32_t id = cluster; ok && id < total; id += clusters) {
       const Tile t = decode<NT, kTile>(a, sh, id);
@@ -887,7 +932,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_narrow(const __grid_constan
       const uint8_t* xq = a.xq + t.x0 / kTile * a.kb * kTileBytes + t.x0 % kTile * kTile;
       const uint8_t* wq = a.wq + t.wtile * a.kb * kTileBytes;
       for (uint32_t kb = k0; kb < k1; ++kb) {
-        if (!(ok = wait_phase(smem_addr(&sh.empty[st.i]), st.phase ^ 1, sh, a.status))) break;
+        if (!(ok = filled < most && wait_phase(smem_addr(&sh.empty[st.i]), st.phase ^ 1, sh, a))) break;
+        if (ahead == 0) ++filled;
         const uint32_t bar = smem_addr(&sh.full[st.i]);
         const uint32_t dst = smem_addr(base + st.i * kStage);
         if (warp == 2) {
@@ -904,7 +950,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_narrow(const __grid_constan
         if (++place == N::kPlaces) place = 0;
       }
     }
-    if (!ok) await_copies(sh, st, kStages);
+    sh.filled[warp / 2] = filled;
   } else if (warp == 1 && lane == 0) {
     // products
     Ring st, tm;
@@ -914,9 +960,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_narrow(const __grid_constan
       uint32_t k0, k1;
       share(t, &k0, &k1);
       for (uint32_t kb = k0; ok && kb < k1; kb += kGroup) {
-        if (!(ok = wait_phase(smem_addr(&sh.tempty[tm.i]), tm.phase ^ 1, sh, a.status))) break;
+        if (!(ok = wait_phase(smem_addr(&sh.tempty[tm.i]), tm.phase ^ 1, sh, a))) break;
         for (uint32_t j = 0; j < kGroup && kb + j < k1; ++j) {
-          if (!(ok = wait_phase(smem_addr(&sh.full[st.i]), st.phase, sh, a.status))) break;
+          if (!(ok = wait_phase(smem_addr(&sh.full[st.i]), st.phase, sh, a))) break;
           fence_after();
           const uint32_t at = smem_addr(base + st.i * kStage);
           issue_block<NT, false>(tmem + tm.i * 128 + j * NT, at, at + kTileBytes);
@@ -928,7 +974,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_narrow(const __grid_constan
         tm.next(2);
       }
     }
-    if (!ok) await_products<false>(sh);
   } else if (warp >= 4) {
     const uint32_t half = (warp - 4) / 4, row = (warp % 4) * 32 + lane;
     const uint32_t taddr = tmem + ((warp % 4) * 32 << 16);
@@ -949,7 +994,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_narrow(const __grid_constan
         if ((kb - k0) % 32 == 0) sw32 = __ldg(wsp + min(kb + lane, k1 - 1));
         const uint32_t n = min(kGroup, k1 - kb);
         const uint32_t j0 = half * (kGroup / 2);  // this half's first block of the group
-        ok = __all_sync(0xffffffffu, wait_phase(smem_addr(&sh.tfull[tm.i]), tm.phase, sh, a.status));
+        ok = __all_sync(0xffffffffu, wait_phase(smem_addr(&sh.tfull[tm.i]), tm.phase, sh, a));
         if (!ok) break;
         fence_after();
 #pragma unroll
@@ -983,8 +1028,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_narrow(const __grid_constan
 
       // Both halves of every block leave their sums in their own shared memory, and each block
       // adds up and stores its share of the columns.
-      ok = __all_sync(0xffffffffu, ranks > 1 ? wait_phase<true>(smem_addr(&sh.pfree), parity ^ 1, sh, a.status)
-                                             : wait_phase(smem_addr(&sh.pfree), parity ^ 1, sh, a.status));
+      ok = __all_sync(0xffffffffu, ranks > 1 ? wait_phase<true>(smem_addr(&sh.pfree), parity ^ 1, sh, a)
+                                             : wait_phase(smem_addr(&sh.pfree), parity ^ 1, sh, a));
       if (!ok) break;
 #pragma unroll
       for (int c = 0; c < NT; ++c) {
@@ -995,10 +1040,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_narrow(const __grid_constan
       __syncwarp();
       if (ranks == 1) {
         if (lane == 0) mbar_arrive(smem_addr(&sh.pfull));
-        ok = __all_sync(0xffffffffu, wait_phase(smem_addr(&sh.pfull), parity, sh, a.status));
+        ok = __all_sync(0xffffffffu, wait_phase(smem_addr(&sh.pfull), parity, sh, a));
       } else {
         if (lane < ranks) peer_arrive(peer_addr(smem_addr(&sh.pfull), lane));
-        ok = __all_sync(0xffffffffu, wait_phase<true>(smem_addr(&sh.pfull), parity, sh, a.status));
+        ok = __all_sync(0xffffffffu, wait_phase<true>(smem_addr(&sh.pfull), parity, sh, a));
       }
       if (!ok) break;
       if (a.dtype == GLEAM_BF16) store_sums<GLEAM_BF16, NT>(a, t, ns.partial, rank, ranks);
@@ -1013,7 +1058,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_narrow(const __grid_constan
       parity ^= 1;
     }
   }
-  finish<false>(tmem, 256, ranks > 1);
+  finish<false>(sh, tmem, 256, ranks > 1, [&] {
+    if (warp == 1 && lane == 0) await_products<false>(sh, 0, true);
+    if (threadIdx.x == 0) await_copies(sh.filled, 2, sh.full, kStages);
+  });
 }
 
 // ---- launches --------------------------------------------------------------

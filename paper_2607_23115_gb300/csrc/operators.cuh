@@ -52,6 +52,8 @@ struct ProductArgs {
   uint32_t w_ready;       // w is not written by the kernel before this one on the stream
   const int32_t *offsets, *counts;
   int32_t* status;
+  unsigned long long wait_ns;
+  uint32_t skip;          // test hook: block 0's first copying thread stops after so many stages
 };
 
 // y = quantised(x) W^T in one launch, for few rows.

@@ -208,6 +208,8 @@ int gleam_fp8_product(const gleam_fp8_product_t* p, gleam_stream_t stream) {
   a.offsets = p->ex.d_offsets;
   a.counts = p->ex.d_counts;
   a.status = p->d_status;
+  a.wait_ns = g_wait_ns.load(std::memory_order_relaxed);
+  a.skip = take_skip();
   return cuda_err(launch_product(a, rows_to_expect(p->m, by_row ? E : 0), reinterpret_cast<cudaStream_t>(stream)));
 }
 
@@ -310,6 +312,8 @@ int gleam_fp8_linear(const gleam_fp8_linear_t* p, gleam_stream_t stream) {
   a.offsets = p->ex.d_offsets;
   a.counts = p->ex.d_counts;
   a.status = p->d_status;
+  a.wait_ns = g_wait_ns.load(std::memory_order_relaxed);
+  a.skip = take_skip();
   return cuda_err(launch_product(a, rows_to_expect(p->rows, E), s));
 }
 
