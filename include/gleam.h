@@ -420,7 +420,8 @@ int gleam_cache_profile_read(gleam_cache_t* cache, double* h_ms, uint64_t* h_lau
  * Value arrays are 16-byte aligned, scale arrays too.
  *
  * The calls are asynchronous on `stream`, run on the current GPU, take device
- * memory only, allocate nothing and keep nothing.  Work that reads or writes
+ * memory only, allocate nothing and keep nothing but what the device found wrong
+ * (gleam_operators_status).  Work that reads or writes
  * their buffers is ordered by the stream: no call lets later work start before
  * its results are written, so they may be the payload of a call with
  * GLEAM_OVERLAP_CALLS. */
@@ -497,7 +498,7 @@ typedef struct gleam_fp8_product {
  * out, and to GLEAM_ERR_INVALID_ARG if an expert's rows lie outside the matrix or
  * start at no multiple of 128 (that expert is left out), or experts share so many
  * rows that they do not fit the matrix (none is computed); otherwise it is not
- * written. */
+ * written.  Where d_status is NULL, the GPU's own word is (gleam_operators_status). */
 int gleam_fp8_product(const gleam_fp8_product_t* p, gleam_stream_t stream);
 
 /* Arguments of gleam_fp8_linear. */
@@ -528,6 +529,11 @@ uint64_t gleam_fp8_linear_work(uint64_t rows, uint64_t cols, uint32_t experts);
  * two add a row's blocks in different orders.  The memory of d_work is free again
  * once the call's work is done. */
 int gleam_fp8_linear(const gleam_fp8_linear_t* p, gleam_stream_t stream);
+
+/* Waits for the work on `stream` and returns what the products on the current GPU without a
+ * d_status have reported since it was last asked: GLEAM_OK, or their last failure, which is
+ * then forgotten.  Not while the stream is captured. */
+int gleam_operators_status(gleam_stream_t stream);
 
 /* Test hooks of the products, for the whole process.  what = GLEAM_DEBUG_WAIT_LIMIT_NS: limit of
  * the waits on the device in nanoseconds (default 4e9).  what = GLEAM_DEBUG_SKIP_ARRIVE: in

@@ -54,7 +54,7 @@ EXPORTS = (
     "gleam_cache_profile", "gleam_cache_profile_read", "gleam_status_string",
     "gleam_fp8_quantize", "gleam_fp8_product", "gleam_fp8_linear", "gleam_fp8_linear_work", "gleam_expert_rows", "gleam_expert_sort",
     "gleam_expert_gather", "gleam_expert_combine", "gleam_expert_combine_grad",
-    "gleam_operators_debug_set",
+    "gleam_operators_status", "gleam_operators_debug_set",
 )
 
 
@@ -159,6 +159,7 @@ def lib() -> ctypes.CDLL:
         "gleam_fp8_linear": (i32, [vp, vp]),
         "gleam_fp8_linear_work": (u64, [u64, u64, u32]),
         "gleam_fp8_product": (i32, [vp, vp]),
+        "gleam_operators_status": (i32, [vp]),
         "gleam_operators_debug_set": (i32, [i32, ctypes.c_int64]),
         "gleam_expert_rows": (u64, [u64, u32, u32, u32]),
         "gleam_expert_sort": (i32, [vp, i32, u64, u32, u32, u32, vp, vp, vp, vp, vp]),
@@ -365,6 +366,10 @@ def gleam_fp8_linear_work(rows: int, cols: int, experts: int = 0) -> int:
 def gleam_fp8_linear(p, stream=None) -> int:
     """p: a gleam_fp8_linear_t."""
     return lib().gleam_fp8_linear(_ref(p), _stream(stream))
+
+
+def gleam_operators_status(stream=None) -> int:
+    return lib().gleam_operators_status(_stream(stream))
 
 
 def gleam_operators_debug_set(what: int, value: int) -> int:

@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_few(const __grid_constant__
           const int32_t o = a.offsets[e], c = a.counts[e];
           const bool bad =
               c != 0 && (o < 0 || c < 0 || (o & (kTile - 1)) != 0 || (uint64_t)o + (uint64_t)c > a.rows);
-          if (bad && a.status != nullptr) *a.status = GLEAM_ERR_INVALID_ARG;
+          if (bad) *a.status = GLEAM_ERR_INVALID_ARG;
           mine = c != 0 && !bad ? slabs : 0;
         }
         uint32_t up = mine;
@@ -321,7 +321,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_few(const __grid_constant__
   }
   // a wait ran out: chunks on their way land before this block's memory goes to another
   if (lane == 0 && !ok) {
-    if (a.status != nullptr) *a.status = GLEAM_ERR_TIMEOUT;
+    *a.status = GLEAM_ERR_TIMEOUT;
     settle_ring(&asked, 1, a.stages, [](uint32_t) {},
                 [&](uint32_t i, uint32_t parity) { mbar_wait(bars + 8 * i, parity, kOperatorWaitNs); });
   }

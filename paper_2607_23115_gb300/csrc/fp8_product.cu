@@ -83,7 +83,7 @@ __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, Contro
     if (t0 == 0) t0 = now;
     if (now - t0 > a.wait_ns) {
       *reinterpret_cast<volatile uint32_t*>(&sh.dead) = 1;
-      if (a.status != nullptr) *a.status = GLEAM_ERR_TIMEOUT;
+      *a.status = GLEAM_ERR_TIMEOUT;
       return false;
     }
   }
@@ -273,7 +273,7 @@ __device__ __forceinline__ void expert_rows(const ProductArgs& a, uint32_t e, ui
   if (c == 0) return;
   if (o < 0 || c < 0 || (o & (kTile - 1)) != 0 || (uint64_t)o + (uint64_t)c > rows) {
     *count = 0;
-    if (a.status != nullptr) *a.status = GLEAM_ERR_INVALID_ARG;
+    *a.status = GLEAM_ERR_INVALID_ARG;
   }
 }
 
@@ -405,7 +405,7 @@ __device__ __forceinline__ void count_tiles(const ProductArgs& a, Control& sh) {
       // more than the rows have room for: experts that share rows, whose tiles may pass 32 bits
       const bool bad = sum > a.tiles;
       if (lane == 0) {
-        if (bad && a.status != nullptr) *a.status = GLEAM_ERR_INVALID_ARG;
+        if (bad) *a.status = GLEAM_ERR_INVALID_ARG;
         sh.total = bad ? 0 : (uint32_t)sum;
       }
     }

@@ -51,7 +51,7 @@ struct ProductArgs {
   uint32_t vec;           // y's rows start 16-byte aligned
   uint32_t w_ready;       // w is not written by the kernel before this one on the stream
   const int32_t *offsets, *counts;
-  int32_t* status;
+  int32_t* status;        // the caller's word, or the GPU's
   unsigned long long wait_ns;
   uint32_t skip;          // test hook: block 0's first copying thread stops after so many stages
 };
@@ -73,7 +73,7 @@ struct FewArgs {
   uint64_t y_ld;          // elements
   uint32_t experts;
   const int32_t *offsets, *counts;
-  int32_t* status;
+  int32_t* status;        // the caller's word, or the GPU's
   unsigned long long wait_ns;
   uint32_t skip;          // test hook: block 0 asks for no chunk after so many (kNoSkip: none)
 };

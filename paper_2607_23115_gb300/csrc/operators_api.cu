@@ -88,6 +88,23 @@ uint32_t take_skip() {
   return g_skip.load(std::memory_order_relaxed) == kNoSkip ? kNoSkip : g_skip.exchange(kNoSkip);
 }
 
+// A failure that the device found, of a product whose caller gave no word for it.
+__device__ int32_t g_failure;
+
+// Its address on the current GPU.
+int failure_word(int dev, int32_t** word) {
+  static std::atomic<int32_t*> known[64] = {};
+  const bool kept = dev >= 0 && dev < 64;
+  *word = kept ? known[dev].load(std::memory_order_relaxed) : nullptr;
+  if (*word != nullptr) return GLEAM_OK;
+  void* p = nullptr;
+  const cudaError_t e = cudaGetSymbolAddress(&p, g_failure);
+  if (e != cudaSuccess) return cuda_err(e);
+  *word = static_cast<int32_t*>(p);
+  if (kept) known[dev].store(*word, std::memory_order_relaxed);
+  return GLEAM_OK;
+}
+
 #define GLEAM_TRY(x)              \
   do {                            \
     const int rc_ = (x);          \
@@ -187,6 +204,9 @@ int gleam_fp8_product(const gleam_fp8_product_t* p, gleam_stream_t stream) {
     if (!aligned(p->d_status, 4)) return GLEAM_ERR_INVALID_ARG;
   }
 
+  int32_t* status = p->d_status;
+  if (status == nullptr) GLEAM_TRY(failure_word(dev, &status));
+
   ProductArgs a{};
   a.xq = p->d_xq;
   a.xs = p->d_xs;
@@ -207,7 +227,7 @@ int gleam_fp8_product(const gleam_fp8_product_t* p, gleam_stream_t stream) {
   a.over = (uint32_t)p->over;
   a.offsets = p->ex.d_offsets;
   a.counts = p->ex.d_counts;
-  a.status = p->d_status;
+  a.status = status;
   a.wait_ns = g_wait_ns.load(std::memory_order_relaxed);
   a.skip = take_skip();
   return cuda_err(launch_product(a, rows_to_expect(p->m, by_row ? E : 0), reinterpret_cast<cudaStream_t>(stream)));
@@ -255,6 +275,8 @@ int gleam_fp8_linear(const gleam_fp8_linear_t* p, gleam_stream_t stream) {
       !aligned(p->ex.d_counts, 4) || !aligned(p->d_status, 4))
     return GLEAM_ERR_INVALID_ARG;
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  int32_t* status = p->d_status;
+  if (status == nullptr) GLEAM_TRY(failure_word(dev, &status));
 
   if (one_kernel(p->rows, x.cols, E)) {
     FewArgs f{};
@@ -277,7 +299,7 @@ int gleam_fp8_linear(const gleam_fp8_linear_t* p, gleam_stream_t stream) {
     f.experts = E;
     f.offsets = p->ex.d_offsets;
     f.counts = p->ex.d_counts;
-    f.status = p->d_status;
+    f.status = status;
     f.wait_ns = g_wait_ns.load(std::memory_order_relaxed);
     f.skip = take_skip();
     return cuda_err(launch_few(f, s));
@@ -311,10 +333,24 @@ int gleam_fp8_linear(const gleam_fp8_linear_t* p, gleam_stream_t stream) {
   a.over = GLEAM_OVER_ROWS;
   a.offsets = p->ex.d_offsets;
   a.counts = p->ex.d_counts;
-  a.status = p->d_status;
+  a.status = status;
   a.wait_ns = g_wait_ns.load(std::memory_order_relaxed);
   a.skip = take_skip();
   return cuda_err(launch_product(a, rows_to_expect(p->rows, E), s));
+}
+
+int gleam_operators_status(gleam_stream_t stream) {
+  const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  int dev = 0;
+  int32_t* word = nullptr;
+  int32_t v = GLEAM_OK;
+  GLEAM_TRY(current_device(&dev));
+  GLEAM_TRY(failure_word(dev, &word));
+  GLEAM_TRY(cuda_err(cudaMemcpyAsync(&v, word, sizeof(v), cudaMemcpyDeviceToHost, s)));
+  GLEAM_TRY(cuda_err(cudaStreamSynchronize(s)));
+  if (v == GLEAM_OK) return GLEAM_OK;
+  GLEAM_TRY(cuda_err(cudaMemsetAsync(word, 0, sizeof(v), s)));
+  return v;
 }
 
 int gleam_operators_debug_set(int what, int64_t value) {

@@ -14,7 +14,7 @@ plan.src_of holds a row's slot, -1 for a row that only fills an expert's last bl
 (include/gleam.h, "tokens by expert").  Rows of no slot are zeros in what gather and
 combine_grad return and are not written by linear and linear_grad; no function here
 reads them.  Weights are fp8.Weight with one matrix per expert.  Streams and errors
-as in module fp8.
+as in module fp8, whose check() also reports a plan whose offsets or counts do not fit its rows.
 """
 from __future__ import annotations
 

@@ -14,7 +14,9 @@ shares.
 Work is enqueued on ``stream`` (a torch.cuda.Stream, its raw handle, or None for
 torch's current stream) of the tensors' GPU; buffers a call needs besides its
 results come from torch's allocator on that stream.  Everything happens in
-libgleam.so; errors raise binding.GleamError.
+libgleam.so; errors raise binding.GleamError.  What only the GPU can find (a plan of other rows
+than the matrix has, a wait that ran out) leaves results unwritten and is kept: check() waits for
+a stream and raises it.
 """
 from __future__ import annotations
 
@@ -44,6 +46,15 @@ _current_device = torch._C._cuda_getDevice
 def _check(rc: int, what: str) -> None:
     if rc < 0:
         raise B.GleamError(rc, what)
+
+
+def check(device=None, stream=None) -> None:
+    """Waits for the work on the stream (default: the GPU's current one) and raises what products on
+    the GPU (default: the current one) have found wrong since it was last called."""
+    with torch.cuda.device(device):
+        if stream is None:
+            stream = torch.cuda.current_stream()
+        _check(B.gleam_operators_status(stream), "fp8.check")
 
 
 def tiles(n: int) -> int:
