@@ -24,7 +24,7 @@ from typing import Optional, Tuple
 import torch
 
 from . import binding as B
-from .fp8 import TILE, Weight, _check, _expect, _linear, _matrix, _On, _product, _quantize, _raw, _rows_of
+from .fp8 import TILE, Weight, _check, _expect, _grad_types, _linear, _matrix, _On, _product, _quantize, _raw, _rows_of
 
 
 class Plan:
@@ -240,13 +240,14 @@ def linear_grad(dh: torch.Tensor, x: torch.Tensor, plan: Plan, w: Weight,
     if dh.shape[1] != w.n or x.shape[1] != w.k:
         raise ValueError("dh %s and x %s do not fit weights [%d, %d]"
                          % (tuple(dh.shape), tuple(x.shape), w.n, w.k))
+    dw_dtype = _grad_types(dh, x, dw_dtype)
     raw = _raw(dh) if stream is None else None
     if raw is None:
         with _On(dh, stream):
             return linear_grad(dh, x, plan, w, dw_dtype, sorted_rows)
     dh, x = _rows_of(dh), _rows_of(x)
     drows = torch.empty((plan.rows, w.k), dtype=dh.dtype, device=dh.device)
-    dw = torch.empty((w.count, w.n, w.k), dtype=dw_dtype or x.dtype, device=dh.device)
+    dw = torch.empty((w.count, w.n, w.k), dtype=dw_dtype, device=dh.device)
     q, s, qt, st = _quantize(raw, dh, plan.rows, w.n, True, True, plan.at_src_of)
     _, _, xq, xs = _quantize(raw, x, plan.rows, w.k, False, True, plan.at_src_of, per_token)
     _product(raw, plan.rows, w.k, w.n, q, s, w.qt, w.st, B.GLEAM_FP8_BLOCKS, drows, plan)

@@ -123,6 +123,16 @@ def _dtype(t: torch.Tensor) -> int:
     return dtype
 
 
+def _grad_types(dy, x, dw_dtype) -> torch.dtype:
+    """dw's type; refuses any that the kernels have not, before there is work."""
+    _dtype(dy)
+    _dtype(x)
+    dw_dtype = dw_dtype or x.dtype
+    if dw_dtype not in DTYPES:
+        raise ValueError("dw_dtype: expected bfloat16, float16 or float32, got %s" % dw_dtype)
+    return dw_dtype
+
+
 def _matrix(t: torch.Tensor) -> bytes:
     """gleam_matrix_t of a [rows, cols] tensor as _rows_of returns it."""
     rows, cols = t.shape
@@ -267,6 +277,7 @@ def linear_grad(dy: torch.Tensor, x: torch.Tensor, w: Weight, dw_dtype: Optional
     if dy.shape[-1] != w.n or x.shape[-1] != w.k or dy.shape[:-1] != x.shape[:-1]:
         raise ValueError("dy %s and x %s do not fit a weight [%d, %d]"
                          % (tuple(dy.shape), tuple(x.shape), w.n, w.k))
+    dw_dtype = _grad_types(dy, x, dw_dtype)
     raw = _raw(dy) if stream is None else None
     if raw is None:
         with _On(dy, stream):
@@ -274,7 +285,7 @@ def linear_grad(dy: torch.Tensor, x: torch.Tensor, w: Weight, dw_dtype: Optional
     d, rows = _rows_of(dy), _rows_of(x)
     m = d.shape[0]
     dx = torch.empty((m, w.k), dtype=dy.dtype, device=dy.device)
-    dw = torch.empty((w.n, w.k), dtype=dw_dtype or x.dtype, device=dy.device)
+    dw = torch.empty((w.n, w.k), dtype=dw_dtype, device=dy.device)
     q, s, qt, st = _quantize(raw, d, m, w.n, True, True)
     _, _, xq, xs = _quantize(raw, rows, m, w.k, False, True)
     _product(raw, m, w.k, w.n, q, s, w.qt, w.st, B.GLEAM_FP8_BLOCKS, dx)
