@@ -24,7 +24,8 @@ from typing import Optional, Tuple
 import torch
 
 from . import binding as B
-from .fp8 import TILE, Weight, _check, _expect, _grad_types, _linear, _matrix, _On, _product, _quantize, _raw, _rows_of
+from .fp8 import (TILE, Weight, _check, _elsewhere, _expect, _grad_types, _linear, _matrix, _product, _quantize,
+                  _raw, _rows_of)
 
 
 class Plan:
@@ -48,6 +49,9 @@ class Plan:
         self._parts, self._buf = (offsets, counts, row_of, src_of), None
         self.at_offsets, self.at_counts = offsets.data_ptr(), counts.data_ptr()
         self.at_row_of, self.at_src_of = row_of.data_ptr(), src_of.data_ptr()
+
+    def _tensors(self):
+        return self._parts if self._buf is None else self._buf
 
     @classmethod
     def _laid_out(cls, experts, align, tokens, per_token, rows, like):
@@ -108,8 +112,7 @@ def sort(ids: torch.Tensor, experts: int, align: int = TILE, stream=None) -> Pla
         raise ValueError("1 .. 1024 experts and a positive alignment")
     raw = _raw(ids) if stream is None else None
     if raw is None:
-        with _On(ids, stream):
-            return sort(ids, experts, align)
+        return _elsewhere(ids, stream, sort, ids, experts, align)
     t, k = ids.shape
     ids = ids.contiguous()
     lib = B.lib()
@@ -144,8 +147,7 @@ def gather(x: torch.Tensor, plan: Plan, stream=None) -> torch.Tensor:
     _tokens(x, plan, "x")
     raw = _raw(x) if stream is None else None
     if raw is None:
-        with _On(x, stream):
-            return gather(x, plan)
+        return _elsewhere(x, stream, gather, x, plan)
     x = _rows_of(x)
     out = torch.empty((plan.rows, x.shape[1]), dtype=x.dtype, device=x.device)
     if out.numel():
@@ -160,8 +162,7 @@ def combine(rows: torch.Tensor, plan: Plan, weights: Optional[torch.Tensor] = No
     _sorted_rows(rows, plan, "rows")
     raw = _raw(rows) if stream is None else None
     if raw is None:
-        with _On(rows, stream):
-            return combine(rows, plan, weights)
+        return _elsewhere(rows, stream, combine, rows, plan, weights)
     rows = _rows_of(rows)
     out = torch.empty((plan.tokens, rows.shape[1]), dtype=rows.dtype, device=rows.device)
     if weights is not None:
@@ -183,8 +184,7 @@ def combine_grad(dy: torch.Tensor, rows: torch.Tensor, plan: Plan, weights: torc
         raise ValueError("dy and rows differ in type or columns")
     raw = _raw(dy) if stream is None else None
     if raw is None:
-        with _On(dy, stream):
-            return combine_grad(dy, rows, plan, weights)
+        return _elsewhere(dy, stream, combine_grad, dy, rows, plan, weights)
     dy, rows, weights = _rows_of(dy), _rows_of(rows), _weights(weights, plan)
     drows = torch.empty((plan.rows, dy.shape[1]), dtype=dy.dtype, device=dy.device)
     dweights = torch.empty_like(weights)
@@ -222,8 +222,7 @@ def linear(x: torch.Tensor, plan: Plan, w: Weight, sorted_rows: bool = False,
         raise ValueError("x has %d columns, the weights %d" % (x.shape[1], w.k))
     raw = _raw(x) if stream is None else None
     if raw is None:
-        with _On(x, stream):
-            return linear(x, plan, w, sorted_rows)
+        return _elsewhere(x, stream, linear, x, plan, w, sorted_rows)
     return _linear(raw, _rows_of(x), w, plan.rows, plan, per_token)
 
 
@@ -243,8 +242,7 @@ def linear_grad(dh: torch.Tensor, x: torch.Tensor, plan: Plan, w: Weight,
     dw_dtype = _grad_types(dh, x, dw_dtype)
     raw = _raw(dh) if stream is None else None
     if raw is None:
-        with _On(dh, stream):
-            return linear_grad(dh, x, plan, w, dw_dtype, sorted_rows)
+        return _elsewhere(dh, stream, linear_grad, dh, x, plan, w, dw_dtype, sorted_rows)
     dh, x = _rows_of(dh), _rows_of(x)
     drows = torch.empty((plan.rows, w.k), dtype=dh.dtype, device=dh.device)
     dw = torch.empty((w.count, w.n, w.k), dtype=dw_dtype, device=dh.device)

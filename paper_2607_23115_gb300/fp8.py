@@ -13,7 +13,8 @@ shares.
 
 Work is enqueued on ``stream`` (a torch.cuda.Stream, its raw handle, or None for
 torch's current stream) of the tensors' GPU; buffers a call needs besides its
-results come from torch's allocator on that stream.  Everything happens in
+results come from torch's allocator on that stream.  A stream that is given is recorded for
+the inputs, and the caller's current one for the results, which wait for nothing by that.  Everything happens in
 libgleam.so; errors raise binding.GleamError.  What only the GPU can find (a plan of other rows
 than the matrix has, a wait that ran out) leaves results unwritten and is kept: check() waits for
 a stream and raises it.
@@ -82,6 +83,9 @@ class Weight:
             _expect(qt, (count, b, a, TILE, TILE), torch.uint8, "qt")
             _expect(st, (count, b, a), torch.float32, "st")
 
+    def _tensors(self):
+        return self.q, self.s, self.qt, self.st
+
 
 def _expect(t, shape, dtype, name):
     if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
@@ -114,6 +118,31 @@ class _On(contextlib.ExitStack):
     def __enter__(self):
         super().__enter__()
         return _current_stream(self.index)
+
+
+def _record(o, stream) -> None:
+    """The memory of tensors, weights and plans is free again only after the stream's work so far."""
+    if isinstance(o, torch.Tensor):
+        o.record_stream(stream)
+    elif isinstance(o, tuple):
+        for part in o:
+            _record(part, stream)
+    elif hasattr(o, "_tensors"):
+        _record(o._tensors(), stream)
+
+
+def _elsewhere(t: torch.Tensor, stream, call, *args):
+    """call(*args) with t's GPU and the stream as torch's current ones.  What goes in was allocated on
+    another stream, and what comes out is the caller's: torch's allocator is told of both."""
+    caller = torch.cuda.current_stream(t.device) if stream is not None and t.is_cuda else None
+    with _On(t, stream):
+        out = call(*args)
+        if caller is not None:
+            mine = torch.cuda.current_stream()
+            if mine != caller:
+                _record(args, mine)
+                _record(out, caller)
+    return out
 
 
 def _dtype(t: torch.Tensor) -> int:
@@ -188,8 +217,7 @@ def quantize_weight(w: torch.Tensor, grad: bool = False, stream=None) -> Weight:
     transpose too, which linear_grad needs."""
     raw = _raw(w) if stream is None else None
     if raw is None:
-        with _On(w, stream):
-            return quantize_weight(w, grad)
+        return _elsewhere(w, stream, quantize_weight, w, grad)
     dim = w.dim()
     if dim not in (2, 3):
         raise ValueError("expected [n, k] or [experts, n, k], got shape %s" % (tuple(w.shape),))
@@ -258,8 +286,7 @@ def linear(x: torch.Tensor, w: Weight, stream=None) -> torch.Tensor:
         raise ValueError("x has %d columns, the weight %d" % (shape[-1], w.k))
     raw = _raw(x) if stream is None else None
     if raw is None:
-        with _On(x, stream):
-            return linear(x, w)
+        return _elsewhere(x, stream, linear, x, w)
     if len(shape) == 2:
         return _linear(raw, _rows_of(x), w, shape[0])
     rows = _rows_of(x)
@@ -280,8 +307,7 @@ def linear_grad(dy: torch.Tensor, x: torch.Tensor, w: Weight, dw_dtype: Optional
     dw_dtype = _grad_types(dy, x, dw_dtype)
     raw = _raw(dy) if stream is None else None
     if raw is None:
-        with _On(dy, stream):
-            return linear_grad(dy, x, w, dw_dtype)
+        return _elsewhere(dy, stream, linear_grad, dy, x, w, dw_dtype)
     d, rows = _rows_of(dy), _rows_of(x)
     m = d.shape[0]
     dx = torch.empty((m, w.k), dtype=dy.dtype, device=dy.device)
