@@ -13,7 +13,8 @@ Slot i = t * per_token + j of a token's j-th expert takes row plan.row_of[t, j];
 plan.src_of holds a row's slot, -1 for a row that only fills an expert's last block
 (include/gleam.h, "tokens by expert").  Rows of no slot are zeros in what gather and
 combine_grad return and are not written by linear and linear_grad; no function here
-reads them.  Weights are fp8.Weight with one matrix per expert.  Streams and errors
+reads them.  Gradients are the calls above: a backward pass through a result to an input that
+requires one raises.  Weights are fp8.Weight with one matrix per expert.  Streams and errors
 as in module fp8, whose check() also reports a plan whose offsets or counts do not fit its rows.
 """
 from __future__ import annotations
@@ -24,8 +25,8 @@ from typing import Optional, Tuple
 import torch
 
 from . import binding as B
-from .fp8 import (TILE, Weight, _check, _elsewhere, _expect, _grad_types, _linear, _matrix, _product, _quantize,
-                  _raw, _rows_of)
+from .fp8 import (TILE, Weight, _check, _elsewhere, _expect, _Explicit, _grad_types, _linear, _matrix, _product,
+                  _quantize, _raw, _rows_of)
 
 
 class Plan:
@@ -148,11 +149,13 @@ def gather(x: torch.Tensor, plan: Plan, stream=None) -> torch.Tensor:
     raw = _raw(x) if stream is None else None
     if raw is None:
         return _elsewhere(x, stream, gather, x, plan)
-    x = _rows_of(x)
+    given, x = x, _rows_of(x)
     out = torch.empty((plan.rows, x.shape[1]), dtype=x.dtype, device=x.device)
     if out.numel():
         _check(B.lib().gleam_expert_gather(_matrix(x), plan.at_src_of, plan.per_token, plan.rows,
                                            out.data_ptr(), raw), "gleam_expert_gather")
+    if given.requires_grad and torch.is_grad_enabled():
+        out = _Explicit.apply("experts.gather", "experts.combine without weights", out, given)
     return out
 
 
@@ -163,7 +166,7 @@ def combine(rows: torch.Tensor, plan: Plan, weights: Optional[torch.Tensor] = No
     raw = _raw(rows) if stream is None else None
     if raw is None:
         return _elsewhere(rows, stream, combine, rows, plan, weights)
-    rows = _rows_of(rows)
+    given, rows = (rows, weights), _rows_of(rows)
     out = torch.empty((plan.tokens, rows.shape[1]), dtype=rows.dtype, device=rows.device)
     if weights is not None:
         weights = _weights(weights, plan)
@@ -172,6 +175,8 @@ def combine(rows: torch.Tensor, plan: Plan, weights: Optional[torch.Tensor] = No
                                             None if weights is None else weights.data_ptr() or None,
                                             plan.tokens, plan.per_token, out.data_ptr(), raw),
                "gleam_expert_combine")
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in given):
+        out = _Explicit.apply("experts.combine", "experts.combine_grad", out, *given)
     return out
 
 
@@ -223,7 +228,10 @@ def linear(x: torch.Tensor, plan: Plan, w: Weight, sorted_rows: bool = False,
     raw = _raw(x) if stream is None else None
     if raw is None:
         return _elsewhere(x, stream, linear, x, plan, w, sorted_rows)
-    return _linear(raw, _rows_of(x), w, plan.rows, plan, per_token)
+    h = _linear(raw, _rows_of(x), w, plan.rows, plan, per_token)
+    if x.requires_grad and torch.is_grad_enabled():
+        h = _Explicit.apply("experts.linear", "experts.linear_grad", h, x)
+    return h
 
 
 def linear_grad(dh: torch.Tensor, x: torch.Tensor, plan: Plan, w: Weight,

@@ -162,6 +162,19 @@ def _grad_types(dy, x, dw_dtype) -> torch.dtype:
     return dw_dtype
 
 
+class _Explicit(torch.autograd.Function):
+    """The result of a call whose gradients are another's: a backward pass that reaches it is told so."""
+
+    @staticmethod
+    def forward(ctx, name, grad, y, *inputs):
+        ctx.message = "%s records no gradient: %s gives it" % (name, grad)
+        return y
+
+    @staticmethod
+    def backward(ctx, *dy):
+        raise RuntimeError(ctx.message)
+
+
 def _matrix(t: torch.Tensor) -> bytes:
     """gleam_matrix_t of a [rows, cols] tensor as _rows_of returns it."""
     rows, cols = t.shape
@@ -278,7 +291,8 @@ def _linear(raw, x, w: Weight, rows, plan=None, per_token=0):
 
 
 def linear(x: torch.Tensor, w: Weight, stream=None) -> torch.Tensor:
-    """y = x W^T for x [..., k], of x's type."""
+    """y = x W^T for x [..., k], of x's type.  Gradients are linear_grad's: a backward pass through y
+    to an x that requires one raises."""
     if w.count != 1:
         _one(w)
     shape = x.shape
@@ -288,9 +302,13 @@ def linear(x: torch.Tensor, w: Weight, stream=None) -> torch.Tensor:
     if raw is None:
         return _elsewhere(x, stream, linear, x, w)
     if len(shape) == 2:
-        return _linear(raw, _rows_of(x), w, shape[0])
-    rows = _rows_of(x)
-    return _linear(raw, rows, w, rows.shape[0]).view(*shape[:-1], w.n)
+        y = _linear(raw, _rows_of(x), w, shape[0])
+    else:
+        rows = _rows_of(x)
+        y = _linear(raw, rows, w, rows.shape[0]).view(*shape[:-1], w.n)
+    if x.requires_grad and torch.is_grad_enabled():
+        y = _Explicit.apply("fp8.linear", "fp8.linear_grad", y, x)
+    return y
 
 
 def linear_grad(dy: torch.Tensor, x: torch.Tensor, w: Weight, dw_dtype: Optional[torch.dtype] = None,
