@@ -184,7 +184,7 @@ def _matrix(t: torch.Tensor) -> bytes:
 def _rows_of(t: torch.Tensor) -> torch.Tensor:
     """[..., K] as a matrix whose rows may be any distance apart; copied only where it is no such."""
     if t.dim() != 2:
-        t = t.reshape(-1, t.shape[-1])
+        t = t.reshape(t.shape[:-1].numel(), t.shape[-1])
     if t.is_contiguous():
         return t
     if ((t.shape[1] > 1 and t.stride(1) != 1) or

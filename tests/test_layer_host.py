@@ -34,3 +34,9 @@ def test_inputs_of_other_types_are_refused(dy, x):
     with pytest.raises(ValueError, match="expected bfloat16"):
         experts.linear_grad(torch.zeros(256, 4, dtype=dy), torch.zeros(5, 6, dtype=x), _plan(2, 5, 2, 256),
                             _weight(2, 4, 6))
+
+
+@pytest.mark.parametrize("shape,rows", [((2, 3, 0), 6), ((0, 4, 0), 0), ((0,), 1), ((5, 0), 5), ((2, 0, 7), 0), ((7,), 1)])
+def test_rows_of_any_shape(shape, rows):
+    """Inputs of no columns too, whose number of rows their size does not tell."""
+    assert fp8._rows_of(torch.zeros(shape)).shape == (rows, shape[-1])
