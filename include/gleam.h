@@ -548,7 +548,8 @@ int gleam_operators_debug_set(int what, int64_t value);
  * ascending order within one, each expert's rows starting at a multiple of
  * `align`. */
 
-/* Rows that `tokens` * `per_token` slots take at most (a multiple of align). */
+/* Rows that `tokens` * `per_token` slots take at most (a multiple of align); 0 for sizes past those that
+ * gleam_expert_sort takes (1024 experts, 2^20 experts of a token, an alignment of 2^20). */
 uint64_t gleam_expert_rows(uint64_t tokens, uint32_t per_token, uint32_t experts, uint32_t align);
 
 /* Sorts the slots: d_offsets i32[experts + 1] (the last: rows in use), d_counts

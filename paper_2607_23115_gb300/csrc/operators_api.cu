@@ -14,6 +14,7 @@ namespace {
 // again.
 constexpr uint64_t kFewRows = 16, kFewRowsOfExpert = 4;
 
+constexpr uint32_t kMaxAlign = 1u << 20, kMaxPerToken = 1u << 20;
 constexpr uint64_t kMaxDim = 0x7fffff00ull;  // rows and columns fit 31 bits, tiles too
 // More than any memory holds, and few enough that spans in bytes stay below 2^63.
 constexpr uint64_t kMaxElements = 1ull << 50, kMaxAllElements = 1ull << 60, kMaxTiles = 1ull << 40;
@@ -367,7 +368,8 @@ int gleam_operators_debug_set(int what, int64_t value) {
 }
 
 uint64_t gleam_expert_rows(uint64_t tokens, uint32_t per_token, uint32_t experts, uint32_t align) {
-  if (align == 0 || tokens > kMaxDim) return 0;
+  if (align == 0 || align > kMaxAlign || tokens > kMaxDim || per_token > kMaxPerToken || experts > kMaxExperts)
+    return 0;
   const uint64_t n = tokens * per_token, most = n < experts ? n : experts;
   return (n + most * (align - 1) + align - 1) / align * align;
 }
@@ -376,7 +378,7 @@ int gleam_expert_sort(const void* d_ids, int id_bytes, uint64_t tokens, uint32_t
                       uint32_t experts, uint32_t align, int32_t* d_offsets, int32_t* d_counts,
                       int32_t* d_row_of, int32_t* d_src_of, gleam_stream_t stream) {
   if ((id_bytes != 4 && id_bytes != 8) || experts == 0 || experts > kMaxExperts || align == 0 ||
-      align > (1u << 20) || tokens > kMaxDim || per_token > (1u << 20))
+      align > kMaxAlign || tokens > kMaxDim || per_token > kMaxPerToken)
     return GLEAM_ERR_INVALID_ARG;
   const uint64_t slots = tokens * per_token, cap = gleam_expert_rows(tokens, per_token, experts, align);
   if (cap > kMaxDim) return GLEAM_ERR_INVALID_ARG;
@@ -441,7 +443,7 @@ int gleam_expert_gather(const gleam_matrix_t* x, const int32_t* d_src_of, uint32
 int gleam_expert_combine(const gleam_matrix_t* rows, const int32_t* d_row_of, const float* d_weights,
                          uint64_t tokens, uint32_t per_token, void* d_out, gleam_stream_t stream) {
   if (rows == nullptr || !shape_ok(*rows) || rows->count != 1 || tokens > kMaxDim ||
-      per_token > (1u << 20))
+      per_token > kMaxPerToken)
     return GLEAM_ERR_INVALID_ARG;
   if (tokens == 0 || rows->cols == 0) return GLEAM_OK;
   const uint64_t size = rows->dtype == GLEAM_FP32 ? 4 : 2, slots = tokens * per_token;
@@ -479,7 +481,7 @@ int gleam_expert_combine_grad(const gleam_matrix_t* dy, const gleam_matrix_t* ro
                               const float* d_weights, uint32_t per_token, void* d_drows,
                               float* d_dweights, gleam_stream_t stream) {
   if (dy == nullptr || rows == nullptr || !shape_ok(*dy) || !shape_ok(*rows) || dy->count != 1 ||
-      rows->count != 1 || dy->dtype != rows->dtype || dy->cols != rows->cols || per_token > (1u << 20))
+      rows->count != 1 || dy->dtype != rows->dtype || dy->cols != rows->cols || per_token > kMaxPerToken)
     return GLEAM_ERR_INVALID_ARG;
   const uint64_t size = dy->dtype == GLEAM_FP32 ? 4 : 2, slots = dy->rows * per_token;
   if (dy->rows + rows->rows == 0) return GLEAM_OK;
