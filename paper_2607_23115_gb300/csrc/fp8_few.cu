@@ -342,7 +342,8 @@ cudaError_t start(const FewArgs& a, cudaStream_t s) {
   b.stages = std::min<uint32_t>(kMaxStages, room / (kWarps * kChunk));
   const uint32_t smem = x + b.stages * kWarps * kChunk;
   // the most that any call takes: another thread's call of the same kernel must not find it lowered
-  if ((e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewMost)) != cudaSuccess) return e;
+  if ((e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewMost)) != cudaSuccess)
+    return e;
   const uint64_t slabs = (a.n + kRows - 1) / kRows;
   // the kernel counts items in 32 bits, whatever the offsets on the device say
   if (std::max<uint64_t>(a.experts, 1) * slabs >= 0x7fffffffull) return cudaErrorInvalidValue;

@@ -245,22 +245,32 @@ __device__ __forceinline__ void peer_expect_tx(uint32_t bar, uint32_t bytes) {
                : "memory");
 }
 
-// The tiles of an operand of a pair's product, as a tensor of three dimensions.  A copy of a tensor,
-// unlike one of bytes, may land in one block and arrive at the other's barrier, so that the first
-// block, which issues the products, waits for the second's copies themselves.  (Told of them
-// by a thread of the second, it takes a release in that thread, 1,100 cycles a stage: 8192 x 14336 x
-// 4096 took 546 us with one such thread, 460 with two.)
+// The tiles of the operands of a pair's product, as tensors of three dimensions, and the scales of their
+// rows, as tensors of two.  A copy of a tensor, unlike one of bytes, may land in one block and arrive
+// at the other's barrier, so that the first block, which issues the products, waits for the second's
+// copies themselves.  (Told of them by a thread of the second, it takes a release in that thread,
+// 1,100 cycles a stage: a call of 8192 x 14336 x 4096 took 546 us with one such thread, 460 with two and
+// takes 383.)  The adding warps know of their scales by the products, as in a block on its own: a
+// barrier of the scales' own to wait for cost the product 6%.
 template <bool kPair>
 struct Maps {};
 template <>
 struct Maps<true> {
-  CUtensorMap x, w;
+  CUtensorMap x, w, xs, ws;
 };
 __device__ __forceinline__ void copy_tile(uint32_t dst, const CUtensorMap* map, uint64_t tile, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], "
       "[%1, {%2, %2, %3}], [%4];" ::"r"(dst),
       "l"(map), "r"(0), "r"((uint32_t)tile), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void copy_scales(uint32_t dst, const CUtensorMap* map, uint64_t row, uint32_t kb,
+                                            uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], "
+      "[%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(map), "r"((uint32_t)row), "r"(kb), "r"(bar)
       : "memory");
 }
 // Rows of expert e (or, over sums, its part of the contraction); none if they lie outside
@@ -497,9 +507,8 @@ struct Wide {
   static constexpr uint32_t kPlaces = kStages + 3;
   struct Shared {
     alignas(16) uint8_t out[kAdders][32 * kOutPitch];
-    alignas(16) float xscales[kPlaces][kTile];
-    alignas(16) float wscales[kPlaces][NT];  // with a scale for each row of w
-    unsigned long long scaled[kPlaces];  // pairs: a place's scales are here
+    alignas(128) float xscales[kPlaces][kTile];
+    alignas(128) float wscales[kPlaces][NT];  // with a scale for each row of w
     Control c;
   };
   static constexpr uint32_t kBytes = 1024 + kStages * kStage + sizeof(Shared);
@@ -609,8 +618,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t rank = kPair ? cluster_rank() : 0;
   const uint32_t id0 = blockIdx.x / kBlocksOfTile, ids = gridDim.x / kBlocksOfTile;
 
-  if (kPair && threadIdx.x == 0)
-    for (uint32_t i = 0; i < W::kPlaces; ++i) mbar_init_n(smem_addr(&ws.scaled[i]), kBlocks ? 1 : 2);
   begin<kPair>(sh, Counts{kStages, 2, kBlocksOfTile * kAdders, 1}, 2 * NT, kPair);
   pdl_wait();
   count_tiles<W::kRows, NT>(a, sh);
@@ -634,42 +641,39 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t xbytes = ((own_rows(t) + 7) & ~7u) * kTile;
         const uint64_t wrow = t.w0 / kTile + rank;  // row tiles of w that exist, of this block's
         const uint32_t wtiles = wrow < a.wrt ? (uint32_t)min((uint64_t)(W::kOwnW / kTile), a.wrt - wrow) : 0;
-        // rows of w that the tile has, for their scales
-        const uint32_t wscales = (uint32_t)min((uint64_t)NT, (a.wrt - t.w0 / kTile) * kTile) * 4;
+        // rows of w whose scales are read; a pair's copy fills up with zeros past the last
+        const uint32_t wscales = kPair ? NT * 4 : (uint32_t)min((uint64_t)NT, (a.wrt - t.w0 / kTile) * kTile) * 4;
         const uint64_t xtile = (t.x0 / kTile + rank) * a.kb, wtile = (t.wtile + rank) * a.kb;
-        const uint32_t values = warp == 0 ? (kPair && xbytes != 0 ? kTileBytes : xbytes) : wtiles * kTileBytes;
-        const uint32_t scales = warp == 0 ? (xbytes != 0 ? kTile * 4 : 0) : (kBlocks ? 0 : wscales);
+        const uint32_t bytes = warp != 0     ? wtiles * kTileBytes + (kBlocks ? 0 : wscales)
+                               : xbytes == 0 ? 0
+                                             : (kPair ? kTileBytes : xbytes) + kTile * 4;
         for (uint32_t kb = t.kb0; kb < t.kb1; ++kb) {
           if (!(ok = filled < most && wait_phase<kPair>(smem_addr(&sh.empty[st.i]), st.phase ^ 1, sh, a))) break;
           ++filled;
           const uint32_t dst = smem_addr(base + st.i * kStage);
-          uint32_t bar = smem_addr(&sh.full[st.i]), scaled = bar;
+          const uint32_t xs = smem_addr(ws.xscales[place]), wsc = smem_addr(ws.wscales[place]);
           if constexpr (kPair) {
-            if (rank == 0) {
-              mbar_expect_tx(bar, values);
+            const uint32_t bar = rank == 0 ? smem_addr(&sh.full[st.i]) : peer_addr(smem_addr(&sh.peer[st.i]), 0);
+            if (rank == 0) mbar_expect_tx(bar, bytes);
+            else peer_expect_tx(bar, bytes);
+            if (warp == 0 && xbytes != 0) {
+              copy_tile(dst, &maps.x, xtile + kb, bar);
+              copy_scales(xs, &maps.xs, t.x0 + rank * kTile, kb, bar);
+            } else if (warp == 2) {
+              if (wtiles != 0) copy_tile(dst + kTileBytes, &maps.w, wtile + kb, bar);
+              if (!kBlocks) copy_scales(wsc, &maps.ws, t.w0, kb, bar);
+            }
+          } else {
+            const uint32_t bar = smem_addr(&sh.full[st.i]);
+            mbar_expect_tx(bar, bytes);
+            if (warp == 0) {
+              copy_in(dst, a.xq + (xtile + kb) * kTileBytes, xbytes, bar);
+              copy_in(xs, a.xs + kb * (a.xrt * kTile) + t.x0, kTile * 4, bar);
             } else {
-              bar = peer_addr(smem_addr(&sh.peer[st.i]), 0);
-              peer_expect_tx(bar, values);
+              for (uint32_t i = 0; i < wtiles; ++i)
+                copy_in(dst + (1 + i) * kTileBytes, a.wq + (wtile + i * a.kb + kb) * kTileBytes, kTileBytes, bar);
+              if (!kBlocks) copy_in(wsc, a.ws + kb * (a.wrt * kTile) + t.w0, wscales, bar);
             }
-            scaled = smem_addr(&ws.scaled[place]);
-            if (warp == 0 || !kBlocks) mbar_expect_tx(scaled, scales);
-          } else {
-            mbar_expect_tx(bar, values + scales);
-          }
-          if (warp == 0) {
-            if (xbytes != 0) {
-              if constexpr (kPair) copy_tile(dst, &maps.x, xtile + kb, bar);
-              else copy_in(dst, a.xq + (xtile + kb) * kTileBytes, xbytes, bar);
-              copy_in(smem_addr(ws.xscales[place]), a.xs + kb * (a.xrt * kTile) + t.x0 + rank * kTile, scales, scaled);
-            }
-          } else {
-            for (uint32_t i = 0; i < wtiles; ++i) {
-              const uint32_t to = dst + (1 + i) * kTileBytes;
-              if constexpr (kPair) copy_tile(to, &maps.w, wtile + kb, bar);
-              else copy_in(to, a.wq + (wtile + i * a.kb + kb) * kTileBytes, kTileBytes, bar);
-            }
-            if (!kBlocks)
-              copy_in(smem_addr(ws.wscales[place]), a.ws + kb * (a.wrt * kTile) + t.w0, scales, scaled);
           }
           st.next(kStages);
           if (++place == W::kPlaces) place = 0;
@@ -709,7 +713,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t taddr = tmem + ((warp % 4) * 32 << 16) + half * kCols;
     // part 0 of tensor memory is free once both blocks' adding warps say so to the first
     const uint32_t tempty = kPair ? peer_addr(smem_addr(&sh.tempty[0]), 0) : smem_addr(&sh.tempty[0]);
-    Ring tm, at;  // at: the block's scales
+    Ring tm;
+    uint32_t place = 0;
     bool ok = true;
     for (uint32_t id = id0; ok && id < total; id += ids) {
       const Tile t = decode<W::kRows, NT>(a, sh, id);
@@ -723,8 +728,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       float sw32 = 0;
       for (uint32_t kb = t.kb0; kb < t.kb1; ++kb) {
         if (kBlocks && (kb - t.kb0) % 32 == 0) sw32 = __ldg(wsp + min(kb + lane, t.kb1 - 1));
-        ok = __all_sync(0xffffffffu, (!kPair || wait_phase(smem_addr(&ws.scaled[at.i]), at.phase, sh, a)) &&
-                                         wait_phase<kPair>(smem_addr(&sh.tfull[tm.i]), tm.phase, sh, a));
+        ok = __all_sync(0xffffffffu, wait_phase<kPair>(smem_addr(&sh.tfull[tm.i]), tm.phase, sh, a));
         if (!ok) break;
         fence_after();
         const uint32_t part = taddr + tm.i * NT;
@@ -732,7 +736,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // registers, the next products may come
         float v[2][kLoad];
         if constexpr (kBlocks) {
-          const float f = ws.xscales[at.i][row] * __shfl_sync(0xffffffffu, sw32, (kb - t.kb0) % 32);
+          const float f = ws.xscales[place][row] * __shfl_sync(0xffffffffu, sw32, (kb - t.kb0) % 32);
           const unsigned long long f2 = pair(f, f);
           tmem_load(part, v[0]);
 #pragma unroll
@@ -758,10 +762,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           unsigned long long f2[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float f = ws.xscales[at.i][(warp % 4) * 32 + lane / 4 + 8 * j];
+            const float f = ws.xscales[place][(warp % 4) * 32 + lane / 4 + 8 * j];
             f2[j] = pair(f, f);
           }
-          const float* s = ws.wscales[at.i] + half * kCols + 2 * (lane % 4);
+          const float* s = ws.wscales[place] + half * kCols + 2 * (lane % 4);
           tmem_load_pieces(part, v[0]);
 #pragma unroll
           for (int c = 0; c < kCols; c += kLoad) {
@@ -789,7 +793,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
         tm.next(2);
-        at.next(W::kPlaces);
+        if (++place == W::kPlaces) place = 0;
       }
       if (!ok) break;
       const uint32_t quarter = (warp % 4) * 32;
@@ -805,13 +809,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     if ((warp == 1 || (W::kTurns && warp == 3)) && lane == 0) await_products<kPair>(sh, warp / 2, rank == 0);
     if (threadIdx.x != 0) return;
     if (rank == 0) await_copies(sh.filled, 2, sh.full, kStages);
-    if constexpr (kPair) {
-      if (rank == 0) {
-        const uint64_t theirs[2] = {peer_load64(peer_addr(smem_addr(&sh.filled[0]), 1)),
-                                    peer_load64(peer_addr(smem_addr(&sh.filled[1]), 1))};
-        await_copies(theirs, 2, sh.peer, kStages);
-      }
-      await_copies(sh.filled, kBlocks ? 1 : 2, ws.scaled, W::kPlaces);
+    if (kPair && rank == 0) {
+      const uint64_t theirs[2] = {peer_load64(peer_addr(smem_addr(&sh.filled[0]), 1)),
+                                  peer_load64(peer_addr(smem_addr(&sh.filled[1]), 1))};
+      await_copies(theirs, 2, sh.peer, kStages);
     }
   });
 }
@@ -1101,17 +1102,26 @@ EncodeFn encode_fn() {
   return fn;
 }
 
-// `tiles` tiles of 128 x 128 bytes, one after the other; a copy takes one.
-cudaError_t map_tiles(CUtensorMap* map, const uint8_t* q, uint64_t tiles) {
+// A tensor of 2 or 3 dimensions without gaps, of which a copy takes a box.
+cudaError_t map_tensor(CUtensorMap* map, const void* d, CUtensorMapDataType type, uint64_t size, uint32_t rank,
+                       const cuuint64_t (&dims)[3], const cuuint32_t (&box)[3]) {
   const EncodeFn fn = encode_fn();
   if (fn == nullptr) return cudaErrorNotSupported;
-  if (tiles > 0x7fffffffull) return cudaErrorInvalidValue;
-  const cuuint64_t dims[3] = {kTile, kTile, tiles}, strides[2] = {kTile, kTileBytes};
-  const cuuint32_t box[3] = {kTile, kTile, 1}, step[3] = {1, 1, 1};
-  const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<uint8_t*>(q), dims, strides, box, step,
+  const cuuint64_t strides[2] = {dims[0] * size, dims[0] * dims[1] * size};
+  const cuuint32_t step[3] = {1, 1, 1};
+  const CUresult r = fn(map, type, rank, const_cast<void*>(d), dims, strides, box, step,
                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+// Tiles, one after the other (coordinates are of 31 bits).
+cudaError_t map_tiles(CUtensorMap* map, const uint8_t* q, uint64_t tiles) {
+  if (tiles > 0x7fffffffull) return cudaErrorInvalidValue;
+  return map_tensor(map, q, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, 3, {kTile, kTile, tiles}, {kTile, kTile, 1});
+}
+// Scales of each row and block of the contraction, those of `rows` rows at a time.
+cudaError_t map_scales(CUtensorMap* map, const float* s, uint64_t row_tiles, uint64_t kb, uint32_t rows) {
+  return map_tensor(map, s, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, 2, {row_tiles * kTile, kb, 1}, {rows, 1, 1});
 }
 
 // Tiles of kX rows of x by kW of w (over rows: at most, as the offsets are on the device).
@@ -1134,8 +1144,11 @@ cudaError_t wide(ProductArgs a, int sms, cudaStream_t s) {
     const uint64_t weights = a.experts != 0 && a.over == GLEAM_OVER_ROWS ? a.experts : 1;
     cudaError_t e = cudaSuccess;
     // without a contraction nothing is copied
-    if (a.kb != 0 && ((e = map_tiles(&maps.x, a.xq, a.xrt * a.kb)) != cudaSuccess ||
-                      (e = map_tiles(&maps.w, a.wq, weights * a.wrt * a.kb)) != cudaSuccess))
+    if (a.kb != 0 &&
+        ((e = map_tiles(&maps.x, a.xq, a.xrt * a.kb)) != cudaSuccess ||
+         (e = map_tiles(&maps.w, a.wq, weights * a.wrt * a.kb)) != cudaSuccess ||
+         (e = map_scales(&maps.xs, a.xs, a.xrt, a.kb, kTile)) != cudaSuccess ||
+         (a.w_form == GLEAM_FP8_GROUPS && (e = map_scales(&maps.ws, a.ws, a.wrt, a.kb, NT)) != cudaSuccess)))
       return e;
   }
   return start(a.w_form == GLEAM_FP8_BLOCKS ? k_fp8_wide<NT, true, kPair> : k_fp8_wide<NT, false, kPair>, W::kBytes,
