@@ -398,7 +398,8 @@ int gleam_cache_profile_read(gleam_cache_t* cache, double* h_ms, uint64_t* h_lau
 /* ---- weights in 8 bits ----------------------------------------------------
  * No counterpart in the paper: what a program does with the weights that this
  * library caches.  Held as e4m3 values with a scale for each block of 128,
- * weights take half the bytes of bf16 to hash, send and cache, and a block of
+ * weights take half the bytes of bf16 to hash, send and cache (as many with their
+ * transposes, which gradients need), and a block of
  * 128 x 128 is one 16 KiB chunk of a cache with that chunk size, so that a
  * change of a weight misses in the chunk of its own block alone.
  *
@@ -490,7 +491,9 @@ typedef struct gleam_fp8_product {
                                 for an expert without rows                            */
 
 /* y = x w^T: y[i, j] = sum over blocks b of x_s[i, b] * w_s[j, b] * sum over the
- * block of x_q[i, :] w_q[j, :], in 32 bits, rounded once to y's type.
+ * block of x_q[i, :] w_q[j, :], in 32 bits, rounded once to y's type.  The two scales are
+ * multiplied first: their product loses bits below 2^-126 (groups whose largest values'
+ * product is under 2^-108) and is infinite from 2^128.
  * With y = x W^T taken as x times W's form, dx = dy W is dy times the form of
  * W^T, and dw = dy^T x is the transposed form of dy times that of x (both
  * GLEAM_FP8_GROUPS).  With experts, offsets are multiples of 128.

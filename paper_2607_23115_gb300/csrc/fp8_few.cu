@@ -9,7 +9,7 @@
 // row) come by bulk copies into a ring of its own, two to six ahead: held in registers, the
 // next ones do not fit beside x's work.  The warps' sums of a slab meet in shared memory and
 // are added in the order of the contraction.  1 x 14336 x 4096: 14.2 us, 4.1 TB/s; 1 x 1024 x
-// 4096: 4.6 us, which is the launch, x's quantisation and the round trips.
+// 4096: 5.3 us, which is the launch, x's quantisation and the round trips.
 //
 // mma.sync pairs byte i of A's and B's registers whatever k they stand for: a lane takes 16
 // neighbouring bytes of a row (its piece of the tile) for four registers of each operand.

@@ -9,8 +9,8 @@
 //
 //   k_fp8_wide    many rows of x: x's rows are the lanes and 128 or 256 rows of w
 //                 the columns.  A lane's factor for a block is then one number,
-//                 x's scale times the weight block's.  8192 x 14336 x 4096: 358 us,
-//                 2,690 TFLOP/s (the library's product with one scale: 3,480), bound by
+//                 x's scale times the weight block's.  8192 x 14336 x 4096: 361 us,
+//                 2,660 TFLOP/s (the library's product with one scale: 3,480), bound by
 //                 the trip of a part of tensor memory to the adding warps and back.
 //   k_fp8_narrow  few rows of x (up to 64): w's rows are the lanes and 16 to 64 rows
 //                 of x the columns, so that nothing is computed for rows that are
@@ -19,8 +19,8 @@
 //                 37 x 14336 x 4096 with its quantisation: 20.6 us, 2.9 TB/s of weights.
 //
 // Both: one block per SM, persistent.  Warps 0 and 2 copy (16 KiB tiles of w, 128 bytes a
-// row of x, each one bulk copy in the order that the tensor cores read), warp 1, in the
-// wide kernel with warp 3, issues the products into two alternating parts of tensor memory,
+// row of x, each one bulk copy, or for a pair's tile a tensor copy, in the order that the tensor
+// cores read), warp 1, in the wide kernel with warp 3, issues the products into two alternating parts of tensor memory,
 // warps 4 to 11 scale, add and store.
 #include <cuda.h>
 
@@ -1184,7 +1184,8 @@ cudaError_t launch_product(const ProductArgs& a, uint64_t rows, cudaStream_t s) 
   if (a.w_form == GLEAM_FP8_BLOCKS && rows <= 128 && 2 * tiles_of(a, 64, kTile) <= (uint64_t)gpu.sms)
     return narrow<64>(a, gpu.sms, s);
   // the tile that takes the least time, counted in waves of tiles over the SMs: at 8192 x 4096 x 4096
-  // a wave of pairs' tiles of 256 x 256 takes 15.5 us, one of 128 x 256 16.9 and one of 128 x 128 12.9
+  // a wave of pairs' tiles of 256 x 256 takes 15.5 us, one of 128 x 256 16.9 and one of 128 x 128 12.9.
+  // The ratio is that of 32 blocks to a tile; starts and stores weigh more with fewer.
   const uint64_t sms = (uint64_t)gpu.sms;
   auto waves = [](uint64_t tiles, uint64_t at_once) { return (tiles + at_once - 1) / at_once; };
   const uint64_t pair = 20 * waves(tiles_of(a, 256, 256), sms / 2), one = 22 * waves(tiles_of(a, 128, 256), sms),
